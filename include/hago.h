@@ -15,6 +15,9 @@
  *   hago_simquant_codes -- simulated_quantize plus its integer codes, one pass
  *   hago_simquant_wrap  -- simulated_quantize with the overflow of the simulated
  *                          integer type (Sec. 5.2)
+ *   hago_mx_quantize, hago_mx_rmsnorm, hago_mx_silu_mul, hago_mx_dense,
+ *   hago_mx_dense_grouped -- microscaled (block-scaled) 4- and 8-bit floating
+ *                          point: a transformer's layers on codes
  * and the operand / accumulator variants the paper names: int16 x int16
  * operands, 24-bit accumulators (Sec. 4.1), shift-only requantize for
  * power-of-two scales (Sec. 5.1).
@@ -79,9 +82,11 @@ typedef enum {
   HAGO_I16 = 2,
   HAGO_I32 = 3,
   HAGO_F32 = 4,
-  HAGO_I24 = 5  /* accumulator type only (Sec. 4.1: accelerators with 24-bit
+  HAGO_I24 = 5, /* accumulator type only (Sec. 4.1: accelerators with 24-bit
                    accumulation): 24-bit two's complement, held sign-extended
                    in an int32; also a simulated type of hago_simquant_wrap */
+  HAGO_BF16 = 6, /* real types of the microscaled operators, beside HAGO_F32:  */
+  HAGO_F16 = 7   /* bfloat16 and IEEE binary16                                 */
 } hago_dtype;
 
 typedef enum {
@@ -397,6 +402,103 @@ hago_status hago_requantize(const void* acc, hago_dtype acc_dtype,
                             int64_t outer, int64_t channels, int64_t inner,
                             const hago_requant* rq, void* out, void* stream);
 
+/*
+ * Microscaled values.  A row of `cols` real numbers is held as codes of 4 bits
+ * (HAGO_MX_FP4: E2M1; magnitudes 0 .5 1 1.5 2 3 4 6) or 8 bits (HAGO_MX_FP8:
+ * E4M3, largest 448) and one scale byte per block of 32 columns (E8M0: byte b
+ * stands for 2^(b - 127), 255 for NaN); a value is its code times its block's
+ * scale.  Rows are held in whole blocks of 128 columns, C = cols rounded up to
+ * 128:
+ *   codes   [rows, C / 2] (two columns a byte, the even one in the lower four
+ *           bits) or [rows, C]; 16-byte aligned
+ *   scales  [rows, C / 32]; 4-byte aligned
+ * Columns behind `cols` hold zero codes, and blocks without a column the scale
+ * byte 0; the products rely on that.
+ * Encoding a block of largest magnitude m: the scale is 2^e with
+ * e = max(floor(log2 m) - emax, -127), emax 2 or 8 (m = 0: e = -127); the code
+ * is the one nearest to x / 2^e, ties to the code with an even last bit,
+ * and the largest one for magnitudes beyond it.  The sign of zero is kept.  A
+ * block that holds a NaN or an infinity gets the scale 255 and zero codes: all
+ * of it stands for NaN.
+ */
+typedef enum { HAGO_MX_FP4 = 0, HAGO_MX_FP8 = 1 } hago_mx_format;
+
+/*
+ * The operators by rows.  x_t: HAGO_F32, HAGO_BF16 or HAGO_F16, the type of
+ * every real tensor of the call; arithmetic is binary32.  x[rows, cols] may
+ * have any row_stride (in elements) of at least its columns; all else is dense.
+ * `values`, unless NULL, takes the values that the codes stand for, rounded to
+ * x_t once, as [rows, cols]: the simulated quantization of the same numbers
+ * (as hago_simquant_codes returns both).
+ *   hago_mx_quantize: codes of x.
+ *   hago_mx_rmsnorm: h = x + residual (NULL: h = x), codes of
+ *     y = h * rsqrt(mean(h^2) + eps) * gamma[col] (NULL: 1), the squares' sum
+ *     in 32 bits per thread and 64 across them; residual_out, unless NULL, takes h rounded to
+ *     x_t (the norm is of h before that rounding).  It may be residual itself,
+ *     or x itself where row_stride == cols.
+ *   hago_mx_silu_mul: x[rows, 2 cols]; codes of g / (1 + exp(-g)) * u with g
+ *     the first cols columns of a row and u the others.
+ * Errors: NULL (x, codes or scales), SHAPE (negative or beyond 2^31 - 129
+ * columns or 2^62 elements, row_stride below the columns), DTYPE (x_t), PARAM
+ * (format; eps negative or not finite; codes, scales misaligned, or a real
+ * tensor that its elements do not align), DEVICE.  Empty tensors are a no-op.
+ */
+hago_status hago_mx_quantize(const void* x, hago_dtype x_t, int64_t rows,
+                             int64_t cols, int64_t row_stride,
+                             hago_mx_format format, void* codes, void* scales,
+                             void* values, void* stream);
+hago_status hago_mx_rmsnorm(const void* x, const void* residual,
+                            const void* gamma, hago_dtype x_t, int64_t rows,
+                            int64_t cols, int64_t row_stride, float eps,
+                            hago_mx_format format, void* residual_out,
+                            void* codes, void* scales, void* values,
+                            void* stream);
+hago_status hago_mx_silu_mul(const void* x, hago_dtype x_t, int64_t rows,
+                             int64_t cols, int64_t row_stride,
+                             hago_mx_format format, void* codes, void* scales,
+                             void* values, void* stream);
+
+/*
+ * Products of microscaled operands: activations a of either format, weights w
+ * of HAGO_MX_FP4, results of out_t (HAGO_F32, HAGO_BF16 or HAGO_F16) rounded
+ * once from a binary32 sum.
+ *   hago_mx_dense:
+ *     out[m,n] = bias[n] + sum_k a[m,k] * w[n,k]       a [M,K], w [N,K]
+ *   hago_mx_dense_grouped (the experts of a layer): T result rows in groups,
+ *     group e = rows offsets[e] .. offsets[e+1] - 1, of its own length, none
+ *     among them:
+ *     out[t,n] = bias[e,n] + sum_k a[r(t),k] * w[e,n,k]
+ *     r(t) = row_index[t], or t where row_index is NULL.  a [a_rows,K],
+ *     w [experts,N,K], offsets [experts + 1] and row_index [T] (device,
+ *     int32), bias [experts,N].  offsets do not decrease and lie in 0..T,
+ *     row_index in 0..a_rows - 1: the caller's contract, as device arrays'
+ *     contents are (other values give wrong results, never an access out of
+ *     bounds).  Rows in no group are not written.  Nothing waits for the
+ *     device: the launch depends on T and experts alone.
+ * bias: device, binary32, or NULL.
+ * 4-bit products are added exactly up to the binary32 rounding of the running
+ * sum.  With 8-bit activations the matrix instruction adds the products of 64
+ * or 128 k aligned to the largest one and cuts off what lies some 2^-17 below
+ * it, far below the step of the codes themselves.
+ * Errors: NULL, SHAPE (negative dimensions, beyond 2^31 - 1, K beyond 2^22,
+ * more than 2^31 - 1 tiles; a_rows == 0 with T > 0; indexed activations of 2^31
+ * bytes and more), DTYPE (out_t), PARAM (format, misaligned operands), DEVICE.
+ * T, M or N == 0 is a no-op, K == 0 yields the bias.
+ */
+hago_status hago_mx_dense(const void* a_codes, const void* a_scales,
+                          hago_mx_format a_format, const void* w_codes,
+                          const void* w_scales, const float* bias, int64_t M,
+                          int64_t N, int64_t K, hago_dtype out_t, void* out,
+                          void* stream);
+hago_status hago_mx_dense_grouped(const void* a_codes, const void* a_scales,
+                                  hago_mx_format a_format, int64_t a_rows,
+                                  const int32_t* row_index,
+                                  const void* w_codes, const void* w_scales,
+                                  const float* bias, const int32_t* offsets,
+                                  int64_t T, int64_t experts, int64_t N,
+                                  int64_t K, hago_dtype out_t, void* out,
+                                  void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* hago_status_string(hago_status s);
 
@@ -445,11 +547,13 @@ hago_status hago_probe_copy(const void* src, void* dst, int64_t bytes,
  *                           (3 is 2)
  *   HAGO_HOOK_GENERAL_TILE  -1 automatic; 0..6 a tile of the general convolution
  *                           kernel (modulo 5: a form of the general dense kernel)
+ *   HAGO_HOOK_MX_KERNEL     -1 automatic; 0.. a kernel of the microscaled products
  * Unknown keys are ignored.
  */
 #define HAGO_HOOK_GEMM_PATH 0
 #define HAGO_HOOK_STREAM_TILE 1
 #define HAGO_HOOK_GENERAL_TILE 2
+#define HAGO_HOOK_MX_KERNEL 3
 void hago_set_test_hook(int32_t key, int32_t value);
 
 #ifdef __cplusplus

@@ -10,7 +10,8 @@ from .binding import (  # noqa: F401
     simquant, simquant_batched, simquant_wrap, requantize, qdense, qconv2d, qconv2d_workspace_bytes, absmax, quantize,
     dequantize, simquant_codes, bit_range, set_test_hook, probe_mfma_i8, probe_copy,
     U8, I8, I16, I32, F32, I24, NCHW, NHWC, STRICT_ACC16, WS_WEIGHTS_READY, STATIC_SCRATCH_BYTES, ROUND_UPWARD, ROUND_HALF_AWAY,
-    HOOK_GEMM_PATH, HOOK_STREAM_TILE, HOOK_GENERAL_TILE,
+    HOOK_GEMM_PATH, HOOK_STREAM_TILE, HOOK_GENERAL_TILE, HOOK_MX_KERNEL,
+    MX, MX_FP4, MX_FP8, BF16, F16, mx_quantize, mx_rmsnorm, mx_silu_mul, mx_dense, mx_dense_grouped,
 )
 
 

@@ -12,11 +12,13 @@ import ctypes as C
 import os
 
 U8, I8, I16, I32, F32, I24 = 0, 1, 2, 3, 4, 5   # I24: accumulator / simulated type only
+BF16, F16 = 6, 7   # real types of the microscaled operators, beside F32
+MX_FP4, MX_FP8 = 0, 1   # hago_mx_format
 NCHW, NHWC = 0, 1
 STRICT_ACC16 = 1
 WS_WEIGHTS_READY = 2
 STATIC_SCRATCH_BYTES = 64 << 20   # HAGO_STATIC_SCRATCH_BYTES
-HOOK_GEMM_PATH, HOOK_STREAM_TILE, HOOK_GENERAL_TILE = 0, 1, 2   # hago_set_test_hook keys
+HOOK_GEMM_PATH, HOOK_STREAM_TILE, HOOK_GENERAL_TILE, HOOK_MX_KERNEL = 0, 1, 2, 3   # hago_set_test_hook keys
 ROUND_UPWARD, ROUND_HALF_AWAY = 0, 1   # hago_rounding
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -24,6 +26,7 @@ _LIB_PATH = os.path.join(_HERE, "libhago.so")
 _NATIVE_PATH = os.path.join(_HERE, "_native.so")
 
 EXPORTS = ("hago_simquant", "hago_simquant_batched", "hago_absmax", "hago_simquant_wrap", "hago_quantize", "hago_dequantize", "hago_simquant_codes", "hago_qdense", "hago_qconv2d", "hago_qconv2d_ws", "hago_qconv2d_workspace_bytes", "hago_qconv2d_static", "hago_requantize",
+           "hago_mx_quantize", "hago_mx_rmsnorm", "hago_mx_silu_mul", "hago_mx_dense", "hago_mx_dense_grouped",
            "hago_status_string", "hago_bit_range", "hago_set_test_hook", "hago_probe_mfma_i8", "hago_probe_copy")
 
 
@@ -94,6 +97,16 @@ def lib():
                                       C.POINTER(_Requant), vp, vp, i64, u32, vp]
         L.hago_qconv2d_workspace_bytes.restype = i64
         L.hago_qconv2d_workspace_bytes.argtypes = [i32, i64, i64, i64, i64, i64, i32, i32, i32, i32, i32, i32, i32]
+        L.hago_mx_quantize.restype = i32
+        L.hago_mx_quantize.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, vp, vp]
+        L.hago_mx_silu_mul.restype = i32
+        L.hago_mx_silu_mul.argtypes = L.hago_mx_quantize.argtypes
+        L.hago_mx_rmsnorm.restype = i32
+        L.hago_mx_rmsnorm.argtypes = [vp, vp, vp, i32, i64, i64, i64, C.c_float, i32, vp, vp, vp, vp, vp]
+        L.hago_mx_dense.restype = i32
+        L.hago_mx_dense.argtypes = [vp, vp, i32, vp, vp, vp, i64, i64, i64, i32, vp, vp]
+        L.hago_mx_dense_grouped.restype = i32
+        L.hago_mx_dense_grouped.argtypes = [vp, vp, i32, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, vp]
         L.hago_bit_range.restype = i32
         L.hago_bit_range.argtypes = [i32, i32, C.POINTER(i32), C.POINTER(i32)]
         L.hago_probe_mfma_i8.restype = i32
@@ -290,3 +303,82 @@ def qconv2d(a, a_t: QType, w, w_t: QType, bias=None, layout=NCHW, stride=(1, 1),
     hago_qconv2d_static."""
     return (_native or _native_module()).qconv2d(a, a_t, w, w_t, bias, layout, stride, pad, groups, acc_dtype, rq, flags, out,
                                                  prepare, workspace, static_scratch)
+
+
+class MX:
+    """A microscaled tensor: codes and scales (uint8 device tensors, laid out as include/hago.h says), the format
+    (MX_FP4 or MX_FP8) and the number of columns that the padded rows stand for."""
+
+    __slots__ = ("codes", "scales", "fmt", "cols")
+
+    def __init__(self, codes, scales, fmt, cols):
+        self.codes, self.scales, self.fmt, self.cols = codes, scales, fmt, cols
+
+    @staticmethod
+    def empty(rows, cols, fmt, device="cuda"):
+        """Room for [rows, cols] (what `out` of the operators below takes)."""
+        import torch
+        wide = (cols + 127) // 128 * 128
+        return MX(torch.empty(rows, wide // 2 if fmt == MX_FP4 else wide, dtype=torch.uint8, device=device),
+                  torch.empty(rows, wide // 32, dtype=torch.uint8, device=device), fmt, cols)
+
+
+def _mx_out(out, fmt, cols):
+    if out is None:
+        return None, None
+    assert out.fmt == fmt and out.cols == cols
+    return out.codes, out.scales
+
+
+def _mx_result(r, prepare, fmt, cols):
+    """The library's (codes, scales, ...) as (MX, ...), or the MX alone."""
+    t = r.out if prepare else r
+    mx = MX(t[0], t[1], fmt, cols)
+    t = mx if len(t) == 2 else (mx, *t[2:])
+    if not prepare:
+        return t
+    r.out = t   # what its calls return
+    return r
+
+
+def mx_quantize(x, fmt, values=False, out=None, prepare=False):
+    """hago_mx_quantize over x[rows, cols] (float32, bfloat16 or float16; rows at any distance): an MX.
+
+    values=True, or a tensor like x to take them: (MX, the values that the codes stand for)."""
+    codes, scales = _mx_out(out, fmt, x.shape[-1])
+    r = (_native or _native_module()).mx_quantize(x, fmt, values, codes, scales, prepare)
+    return _mx_result(r, prepare, fmt, x.shape[-1])
+
+
+def mx_rmsnorm(x, gamma=None, residual=None, eps=1e-5, fmt=MX_FP8, values=False, out=None, out_residual=None, prepare=False):
+    """hago_mx_rmsnorm over x[rows, cols]: an MX of the norm of x, or with a residual (MX, x + residual).
+
+    out_residual: the tensor to take the sum, which may be `residual` itself; values as in mx_quantize, returned last."""
+    codes, scales = _mx_out(out, fmt, x.shape[-1])
+    keep = out_residual if out_residual is not None else residual is not None
+    r = (_native or _native_module()).mx_rmsnorm(x, gamma, residual, eps, fmt, values, codes, scales, keep, prepare)
+    return _mx_result(r, prepare, fmt, x.shape[-1])
+
+
+def mx_silu_mul(x, fmt, values=False, out=None, prepare=False):
+    """hago_mx_silu_mul over x[rows, 2 cols], gate and up side by side: an MX of silu(gate) * up; values as in mx_quantize."""
+    cols = x.shape[-1] // 2
+    codes, scales = _mx_out(out, fmt, cols)
+    r = (_native or _native_module()).mx_silu_mul(x, fmt, values, codes, scales, prepare)
+    return _mx_result(r, prepare, fmt, cols)
+
+
+def mx_dense(a: MX, w: MX, bias=None, out_dtype=BF16, out=None, prepare=False):
+    """hago_mx_dense: a [M,K] (either format), w [N,K] (MX_FP4), bias [N] float32 -> [M,N] of out_dtype (BF16, F16, F32)."""
+    assert w.fmt == MX_FP4 and a.cols == w.cols
+    return (_native or _native_module()).mx_dense(a.codes, a.scales, a.fmt, w.codes, w.scales, a.cols, bias, out_dtype, out, prepare)
+
+
+def mx_dense_grouped(a: MX, w: MX, offsets, rows=None, bias=None, out_dtype=BF16, out=None, prepare=False):
+    """hago_mx_dense_grouped: w [E,N,K] (codes and scales with that axis in front), offsets [E + 1] int32 on the device.
+
+    Result row t belongs to the group e with offsets[e] <= t < offsets[e + 1] and is made of a's row rows[t] (int32
+    device tensor; None: row t); bias [E,N] float32.  Returns [T,N]; rows in no group are not written."""
+    assert w.fmt == MX_FP4 and a.cols == w.cols
+    return (_native or _native_module()).mx_dense_grouped(a.codes, a.scales, a.fmt, w.codes, w.scales, a.cols, offsets, rows, bias, out_dtype, out,
+                                                          prepare)

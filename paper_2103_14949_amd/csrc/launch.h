@@ -143,8 +143,9 @@ hipError_t launch_conv_prepack(const GemmArgs& g, const ConvGeom& cg, int32_t Cp
 // The weight part alone.
 hipError_t launch_conv_prepack_weights(const GemmArgs& g, const ConvGeom& cg, int32_t Cp, int8_t* wgt_out, hipStream_t st);
 // Test hooks (see hago_set_test_hook): which GEMM kernel family and tile serve the next calls.
-enum { kHookGemmPath = 0, kHookDmaTile = 1, kHookGenericTile = 2, kNumHooks = 3 };
+enum { kHookGemmPath = 0, kHookDmaTile = 1, kHookGenericTile = 2, kHookMxKernel = 3, kNumHooks = 4 };
 void set_test_hook(int key, int value);
+int test_hook(int key);
 // 3x3 stride-1 pad-1 NCHW convolution in one launch, no scratch; false when the geometry is not
 // that kernel's (nothing is launched then).
 bool try_qconv3x3_nchw(const GemmArgs& g, const ConvGeom& cg, hipStream_t st, hipError_t* err);

@@ -1,0 +1,85 @@
+// Pieces shared by the microscaled matrix products: which rows a tile has, and how results leave.
+#pragma once
+
+#include "mx_device.h"
+
+namespace hago {
+
+typedef int mx_v4i __attribute__((ext_vector_type(4)));
+typedef int mx_v8i __attribute__((ext_vector_type(8)));
+typedef float mx_v4f __attribute__((ext_vector_type(4)));
+typedef float mx_v16f __attribute__((ext_vector_type(16)));
+
+// cbsz / blgp of the scaled matrix instructions
+template <int FORMAT>
+constexpr int kMxMfmaFormat = FORMAT == kMxFp4 ? 4 : 0;
+
+// Rows [row, end) of a group, in tiles of ROWS.
+struct MxRows {
+  int expert, row, end;
+};
+
+// One wavefront's look at 64 groups: lane l has group first + l.  The tiles of this and the groups before it are counted up.
+struct MxScan {
+  int lo, hi, upto, here;
+};
+template <int ROWS>
+__device__ __forceinline__ MxScan mx_scan(const int32_t* offsets, int T, int experts, int first, int before) {
+  const int lane = (int)threadIdx.x & 63, e = first + lane;
+  MxScan s{0, 0, 0, 0};
+  if (e < experts) {
+    // (what lies outside the rows is none of theirs, whatever the array holds)
+    s.lo = min(max(offsets[e], 0), T);
+    s.hi = min(max(offsets[e + 1], s.lo), T);
+    s.here = (int)((uint32_t)(s.hi - s.lo + ROWS - 1) / ROWS);
+  }
+  s.upto = s.here;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(s.upto, d);
+    if (lane >= d) s.upto += o;
+  }
+  s.upto += before;
+  return s;
+}
+
+// Tile `pick(number of tiles)` of the groups' rows; false: pick gave none (a negative number, or one beyond them).  pick is called once, with a uniform number.
+template <int ROWS, typename Pick>
+__device__ __forceinline__ bool mx_find_rows(const MxGemmArgs& g, const Pick& pick, MxRows& rows) {
+  if (!g.offsets) {
+    const int tile = pick((int)((uint32_t)(g.T + ROWS - 1) / ROWS));
+    rows = {0, tile * ROWS, g.T};
+    return tile >= 0 && rows.row < g.T;
+  }
+  auto last = [](int v) { return __builtin_amdgcn_readlane(v, 63); };
+  MxScan s = mx_scan<ROWS>(g.offsets, g.T, g.experts, 0, 0);
+  int total = last(s.upto);
+  for (int first = 64; first < g.experts; first += 64) total = last(mx_scan<ROWS>(g.offsets, g.T, g.experts, first, total).upto);
+  const int tile = pick(total);
+  if (tile < 0 || tile >= total) return false;
+  for (int first = 0;; first += 64) {
+    if (first) s = mx_scan<ROWS>(g.offsets, g.T, g.experts, first, last(s.upto));
+    const uint64_t there = __ballot(tile < s.upto);
+    if (there) {
+      const int l = __builtin_ctzll(there);
+      const int lo = __builtin_amdgcn_readlane(s.lo, l), upto = __builtin_amdgcn_readlane(s.upto, l), here = __builtin_amdgcn_readlane(s.here, l);
+      rows = {first + l, lo + (tile - (upto - here)) * ROWS, __builtin_amdgcn_readlane(s.hi, l)};
+      return true;
+    }
+  }
+}
+
+// The row of A that result row t is made of.
+__device__ __forceinline__ int mx_row_of(const MxGemmArgs& g, int t) {
+  if (!g.index) return t;
+  const int r = g.index[t];
+  return min(max(r, 0), g.a_rows - 1);  // (in bounds whatever the array holds)
+}
+
+__device__ __forceinline__ void mx_store_one(void* out, int type, int64_t at, float v) {
+  if (type == kMxF32) static_cast<float*>(out)[at] = v;
+  else if (type == kMxBf16) static_cast<__bf16*>(out)[at] = (__bf16)v;
+  else static_cast<_Float16*>(out)[at] = (_Float16)v;
+}
+
+}  // namespace hago

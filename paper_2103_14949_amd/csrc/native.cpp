@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -23,7 +24,8 @@ namespace {
 #define HAGO_ENTRIES(X)                                                                                            \
   X(hago_simquant) X(hago_simquant_wrap) X(hago_simquant_batched) X(hago_quantize) X(hago_dequantize)              \
   X(hago_simquant_codes) X(hago_absmax) X(hago_requantize) X(hago_qdense) X(hago_qconv2d) X(hago_qconv2d_ws)       \
-  X(hago_qconv2d_static) X(hago_bit_range)
+  X(hago_qconv2d_static) X(hago_bit_range) X(hago_mx_quantize) X(hago_mx_rmsnorm) X(hago_mx_silu_mul)                 \
+  X(hago_mx_dense) X(hago_mx_dense_grouped)
 struct Library {
 #define X(name) decltype(&::name) name;
   HAGO_ENTRIES(X)
@@ -105,6 +107,8 @@ at::ScalarType scalar_type(int64_t code) {
     case HAGO_I16: return at::kShort;
     case HAGO_I32: case HAGO_I24: return at::kInt;
     case HAGO_F32: return at::kFloat;
+    case HAGO_BF16: return at::kBFloat16;
+    case HAGO_F16: return at::kHalf;
   }
   PyErr_SetObject(PyExc_KeyError, PyLong_FromLongLong(code));
   throw Raised{};
@@ -570,6 +574,179 @@ PyObject* f_qconv2d(PyObject* const* a, Py_ssize_t n) {
                out, prepare, {a[0], a[2], a[4], tensors.mult.o, tensors.shift.o});
 }
 
+// ---- microscaled operators
+// The tensors of a call lie on the device that it is issued on (the library takes addresses of that one only).
+void on_current_device(std::initializer_list<PyObject*> tensors) {
+  for (PyObject* o : tensors)
+    if (o && o != Py_None) require(tensor(o).is_cuda() && tensor(o).get_device() == c10::hip::current_device());
+}
+hago_dtype real_type(const at::Tensor& t) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return HAGO_F32;
+    case at::kBFloat16: return HAGO_BF16;
+    case at::kHalf: return HAGO_F16;
+    default: PyErr_SetString(PyExc_TypeError, "a float32, bfloat16 or float16 tensor is needed"); throw Raised{};
+  }
+}
+// A tensor that the caller gave, of this shape and type; None is left alone.
+void given(PyObject* o, at::IntArrayRef shape, at::ScalarType type) {
+  if (o == Py_None) return;
+  const at::Tensor& t = tensor(o);
+  require(t.sizes() == shape && t.scalar_type() == type && t.is_contiguous());
+}
+int64_t mx_padded(int64_t cols) { return (cols + 127) / 128 * 128; }
+int64_t mx_code_bytes(int64_t cols, int64_t format) { return format == HAGO_MX_FP4 ? mx_padded(cols) / 2 : mx_padded(cols); }
+void require_format(int64_t f) { require(f == HAGO_MX_FP4 || f == HAGO_MX_FP8); }
+
+struct MxRows {  // x[rows, columns], rows at any distance
+  hago_dtype type;
+  at::ScalarType scalar;
+  int64_t rows, columns, stride;
+  const void* src;
+};
+MxRows mx_rows(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  require(t.dim() == 2);
+  const int64_t rows = t.size(0), columns = t.size(1);
+  require(t.numel() == 0 || ((columns <= 1 || t.stride(1) == 1) && (rows <= 1 || t.stride(0) >= columns)));
+  return {real_type(t), t.scalar_type(), rows, columns, rows > 1 && columns ? t.stride(0) : columns, t.data_ptr()};
+}
+
+// What such an operator returns, as a tuple: codes, scales, then the residual and the values where they are asked for.
+// `values` is None, True or the tensor to take them.
+struct MxResults {
+  PyObject* all;
+  void *codes, *scales, *residual = nullptr, *values = nullptr;
+};
+MxResults mx_results(const at::Tensor& like, const MxRows& x, int64_t cols, int64_t format, PyObject* codes, PyObject* scales, PyObject* residual, PyObject* values) {
+  require_format(format);
+  const int64_t code_shape[2] = {x.rows, mx_code_bytes(cols, format)}, scale_shape[2] = {x.rows, mx_padded(cols) / 32}, shape[2] = {x.rows, cols};
+  given(codes, at::IntArrayRef(code_shape, 2), at::kByte);
+  given(scales, at::IntArrayRef(scale_shape, 2), at::kByte);
+  const bool has_residual = residual != Py_False, has_values = values != Py_None && values != Py_False;
+  if (residual != Py_True && has_residual) given(residual, at::IntArrayRef(shape, 2), x.scalar);
+  if (values != Py_True && has_values) given(values, at::IntArrayRef(shape, 2), x.scalar);
+  PyObject* all = PyTuple_New(2 + has_residual + has_values);
+  if (!all) throw Raised{};
+  try {
+    Py_ssize_t i = 0;
+    auto add = [&](PyObject* o, const int64_t* s, at::ScalarType type) {
+      PyObject* t = output(o == Py_True ? Py_None : o, at::IntArrayRef(s, 2), type, like);
+      PyTuple_SET_ITEM(all, i++, t);
+      return tensor(t).data_ptr();
+    };
+    MxResults r{all, add(codes, code_shape, at::kByte), nullptr};
+    r.scales = add(scales, scale_shape, at::kByte);
+    if (has_residual) r.residual = add(residual, shape, x.scalar);
+    if (has_values) r.values = add(values, shape, x.scalar);
+    return r;
+  } catch (...) {
+    Py_DECREF(all);
+    throw;
+  }
+}
+
+// mx_quantize, mx_silu_mul: (x, format, values, codes, scales, prepare)
+template <class Fn>
+PyObject* mx_quantize_with(Fn fn, bool gated, PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 6);
+  const MxRows x = mx_rows(a[0]);
+  const int64_t format = as_int(a[1]);
+  require(!gated || x.columns % 2 == 0);
+  const int64_t cols = gated ? x.columns / 2 : x.columns;
+  on_current_device({a[0], a[2] == Py_True || a[2] == Py_False ? nullptr : a[2], a[3], a[4]});
+  const bool prepare = as_bool(a[5]);
+  void* st = stream();
+  const MxResults r = mx_results(tensor(a[0]), x, cols, format, a[3], a[4], Py_False, a[2]);
+  return issue([=] { return fn(x.src, x.type, x.rows, cols, x.stride, (hago_mx_format)format, r.codes, r.scales, r.values, st); }, r.all, prepare, {a[0]});
+}
+PyObject* f_mx_quantize(PyObject* const* a, Py_ssize_t n) { return mx_quantize_with(L.hago_mx_quantize, false, a, n); }
+PyObject* f_mx_silu_mul(PyObject* const* a, Py_ssize_t n) { return mx_quantize_with(L.hago_mx_silu_mul, true, a, n); }
+
+// (x, gamma, residual, eps, format, values, codes, scales, out_residual, prepare); out_residual: False where none is wanted
+PyObject* f_mx_rmsnorm(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 10);
+  const MxRows x = mx_rows(a[0]);
+  const int64_t shape[2] = {x.rows, x.columns};
+  given(a[1], at::IntArrayRef(&x.columns, 1), x.scalar);
+  given(a[2], at::IntArrayRef(shape, 2), x.scalar);
+  const double eps = PyFloat_AsDouble(a[3]);
+  if (eps == -1.0 && PyErr_Occurred()) throw Raised{};
+  const int64_t format = as_int(a[4]);
+  auto maybe = [](PyObject* o) { return o == Py_True || o == Py_False ? nullptr : o; };
+  on_current_device({a[0], a[1], a[2], maybe(a[5]), a[6], a[7], maybe(a[8])});
+  const void *gamma = pointer(a[1]), *res = pointer(a[2]);
+  const bool prepare = as_bool(a[9]);
+  void* st = stream();
+  const MxResults r = mx_results(tensor(a[0]), x, x.columns, format, a[6], a[7], a[8], a[5]);
+  return issue([=] { return L.hago_mx_rmsnorm(x.src, res, gamma, x.type, x.rows, x.columns, x.stride, (float)eps, (hago_mx_format)format, r.residual, r.codes,
+                                              r.scales, r.values, st); },
+               r.all, prepare, {a[0], a[1], a[2]});
+}
+
+struct MxOperand {
+  const void *codes, *scales;
+  int64_t rows;
+};
+// codes and scales of [.., rows, cols] in a format
+MxOperand mx_operand(PyObject* codes, PyObject* scales, int64_t dims, int64_t cols, int64_t format) {
+  require_format(format);
+  require(cols >= 0);
+  const at::Tensor &c = tensor(codes), &s = tensor(scales);
+  require(c.dim() == dims && s.dim() == dims && c.scalar_type() == at::kByte && s.scalar_type() == at::kByte && c.is_contiguous() && s.is_contiguous());
+  require(c.size(dims - 1) == mx_code_bytes(cols, format) && s.size(dims - 1) == mx_padded(cols) / 32 && c.size(dims - 2) == s.size(dims - 2));
+  require(dims == 2 || c.size(0) == s.size(0));
+  return {c.data_ptr(), s.data_ptr(), c.size(dims - 2)};
+}
+
+// (a_codes, a_scales, a_format, w_codes, w_scales, cols, bias, out_dtype, out, prepare)
+PyObject* f_mx_dense(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 10);
+  const int64_t format = as_int(a[2]), K = as_int(a[5]), type = as_int(a[7]);
+  const MxOperand act = mx_operand(a[0], a[1], 2, K, format), w = mx_operand(a[3], a[4], 2, K, HAGO_MX_FP4);
+  const int64_t M = act.rows, N = w.rows, shape[2] = {M, N};
+  given(a[6], at::IntArrayRef(&N, 1), at::kFloat);
+  given(a[8], at::IntArrayRef(shape, 2), scalar_type(type));
+  on_current_device({a[0], a[1], a[3], a[4], a[6], a[8]});
+  const float* bias = static_cast<const float*>(pointer(a[6]));
+  const bool prepare = as_bool(a[9]);
+  void* st = stream();
+  PyObject* out = output(a[8], at::IntArrayRef(shape, 2), scalar_type(type), tensor(a[0]));
+  void* dst = pointer(out);
+  return issue([=] { return L.hago_mx_dense(act.codes, act.scales, (hago_mx_format)format, w.codes, w.scales, bias, M, N, K, (hago_dtype)type, dst, st); }, out,
+               prepare, {a[0], a[1], a[3], a[4], a[6]});
+}
+
+// (a_codes, a_scales, a_format, w_codes, w_scales, cols, offsets, rows, bias, out_dtype, out, prepare)
+PyObject* f_mx_dense_grouped(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 12);
+  const int64_t format = as_int(a[2]), K = as_int(a[5]), type = as_int(a[9]);
+  const MxOperand act = mx_operand(a[0], a[1], 2, K, format), w = mx_operand(a[3], a[4], 3, K, HAGO_MX_FP4);
+  const int64_t E = tensor(a[3]).size(0), N = w.rows, entries = E + 1, bias_shape[2] = {E, N};
+  tensor(a[6]);
+  given(a[6], at::IntArrayRef(&entries, 1), at::kInt);
+  int64_t T = act.rows;
+  if (a[7] != Py_None) {
+    require(tensor(a[7]).dim() == 1);
+    T = tensor(a[7]).size(0);
+    given(a[7], at::IntArrayRef(&T, 1), at::kInt);
+  }
+  const int64_t shape[2] = {T, N};
+  given(a[8], at::IntArrayRef(bias_shape, 2), at::kFloat);
+  given(a[10], at::IntArrayRef(shape, 2), scalar_type(type));
+  on_current_device({a[0], a[1], a[3], a[4], a[6], a[7], a[8], a[10]});
+  const int32_t *offsets = static_cast<const int32_t*>(pointer(a[6])), *index = static_cast<const int32_t*>(pointer(a[7]));
+  const float* bias = static_cast<const float*>(pointer(a[8]));
+  const bool prepare = as_bool(a[11]);
+  const int64_t a_rows = act.rows;
+  void* st = stream();
+  PyObject* out = output(a[10], at::IntArrayRef(shape, 2), scalar_type(type), tensor(a[0]));
+  void* dst = pointer(out);
+  return issue([=] { return L.hago_mx_dense_grouped(act.codes, act.scales, (hago_mx_format)format, a_rows, index, w.codes, w.scales, bias, offsets, T, E, N, K,
+                                                    (hago_dtype)type, dst, st); },
+               out, prepare, {a[0], a[1], a[3], a[4], a[6], a[7], a[8]});
+}
+
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -622,7 +799,8 @@ PyObject* f_entries(PyObject* const*, Py_ssize_t n) {
 PyMethodDef methods[] = {HAGO_METHOD(bind), HAGO_METHOD(entries), HAGO_METHOD(simquant), HAGO_METHOD(simquant_wrap),
                          HAGO_METHOD(simquant_batched), HAGO_METHOD(quantize), HAGO_METHOD(simquant_codes),
                          HAGO_METHOD(dequantize), HAGO_METHOD(absmax), HAGO_METHOD(requantize), HAGO_METHOD(qdense),
-                         HAGO_METHOD(qconv2d), {}};
+                         HAGO_METHOD(qconv2d), HAGO_METHOD(mx_quantize), HAGO_METHOD(mx_silu_mul), HAGO_METHOD(mx_rmsnorm),
+                         HAGO_METHOD(mx_dense), HAGO_METHOD(mx_dense_grouped), {}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native marshalling of the libhago binding.", -1, methods};
 
 }  // namespace

@@ -401,7 +401,7 @@ double shape_cost(const TileShape& s, int64_t P_ext, int64_t Q_ext, int64_t K) {
 }
 
 // Test hooks: -1 / 0 mean "choose automatically".  Plain atomics: a test sets them between calls.
-std::atomic<int> g_hook[kNumHooks] = {0, -1, -1};
+std::atomic<int> g_hook[kNumHooks] = {0, -1, -1, -1};
 
 int pick_shape(int mode, int64_t P_ext, int64_t Q_ext, int64_t K) {
   const int v = g_hook[kHookGenericTile].load(std::memory_order_relaxed);  // forced tile (tests)
@@ -428,6 +428,8 @@ extern "C" void hago_debug_set_stamp_buffer(long long* buf, int skip) {
   g_stamp_skip = skip;
 }
 #endif
+
+int test_hook(int key) { return g_hook[key].load(std::memory_order_relaxed); }
 
 void set_test_hook(int key, int value) {
   if (key >= 0 && key < kNumHooks) g_hook[key].store(value, std::memory_order_relaxed);
