@@ -5,57 +5,32 @@
 // of k = 32 (l / 32) on, of 8-bit codes the 16 bytes of k = 16 (l / 32) on and those of k = 32 + 16 (l / 32) on; the scale that lane l
 // gives is the one of k = 32 (l / 32) on of its row.  Products of two 4-bit codes are added exactly (2e-8 of the terms' sum against 64
 // bits).  Of 8-bit codes the instruction adds terms aligned to the largest one, and what lies some 2^-17 below it is cut off.
-#include "mx_gemm.h"
+#include "mx_tile.h"
 
 namespace hago {
 
 namespace {
 
-// One wavefront per 32 x 32 tile, operands straight from memory.
+// Tiles BP x BQ (features x rows) by number, the largest one first.
 template <int FA>
-__global__ __launch_bounds__(64) void mx_gemm_simple_kernel(MxGemmArgs g) {
-  const int lane = threadIdx.x, half = lane >> 5;
-  const int tiles_p = (g.N + 31) / 32;
-  const int tile_p = (int)(blockIdx.x % (uint32_t)tiles_p), tile_q = (int)(blockIdx.x / (uint32_t)tiles_p);
-  MxRows rows;
-  if (!mx_find_rows<32>(g, [&](int) { return tile_q; }, rows)) return;
-  const int padded = (g.K + 127) & ~127;
-  const int t = rows.row + (lane & 31);
-  const int64_t ra = mx_row_of(g, min(t, rows.end - 1));
-  const int64_t rw = (int64_t)rows.expert * g.N + min(tile_p * 32 + (lane & 31), g.N - 1);
-  const uint8_t* a = g.a + ra * (FA == kMxFp4 ? padded / 2 : padded) + half * 16;
-  const uint8_t* w = g.w + rw * (padded / 2) + half * 16;
-  const uint8_t* as = g.a_scale + ra * (padded / 32) + half;
-  const uint8_t* ws = g.w_scale + rw * (padded / 32) + half;
-  mx_v16f acc = {};
-  for (int k = 0; k < padded; k += 64) {
-    mx_v8i p = {}, q = {};
-    const mx_v4i wv = *reinterpret_cast<const mx_v4i*>(w + k / 2);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = wv[i];
-    const mx_v4i lo = *reinterpret_cast<const mx_v4i*>(a + (FA == kMxFp4 ? k / 2 : k));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = lo[i];
-    if constexpr (FA == kMxFp8) {
-      const mx_v4i hi = *reinterpret_cast<const mx_v4i*>(a + k + 32);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) q[4 + i] = hi[i];
-    }
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc, kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 0, ws[k / 32], 0, as[k / 32]);
+hipError_t launch_shape(const MxGemmArgs& g, int shape, hipStream_t st) {
+  switch (shape) {
+    case 0: return FA == kMxFp4 ? launch_tile<kMxFp4, 2, 4, 4, 2>(g, st) : launch_tile<kMxFp8, 4, 2, 2, 2>(g, st);  // 256 x 256, 256 x 128
+    case 1: return launch_tile<FA, 2, 2, 2, 2>(g, st);                                                             // 128 x 128
+    default: return launch_tile<FA, 2, 2, 1, 1>(g, st);                                                            // 64 x 64
   }
-  if (t >= rows.end) return;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int n = tile_p * 32 + 8 * (r / 4) + 4 * half + r % 4;
-    if (n < g.N) mx_store_one(g.out, g.type, (int64_t)t * g.N + n, g.bias ? acc[r] + g.bias[(int64_t)rows.expert * g.N + n] : acc[r]);
-  }
+}
+
+int64_t count_tiles(const MxGemmArgs& g, int bp, int bq) {
+  return (int64_t)((g.N + bp - 1) / bp) * (g.offsets ? mx_most_tiles(g.T, g.experts, bq) : (g.T + bq - 1) / bq);
 }
 
 }  // namespace
 
 hipError_t launch_mx_gemm(const MxGemmArgs& g, int a_format, hipStream_t st) {
-  const int64_t tiles = (int64_t)((g.N + 31) / 32) * (g.offsets ? mx_most_tiles(g.T, g.experts, 32) : (g.T + 31) / 32);
-  return launch_kernel(a_format == kMxFp4 ? mx_gemm_simple_kernel<kMxFp4> : mx_gemm_simple_kernel<kMxFp8>, dim3((unsigned)tiles), dim3(64), 0, st, g);
+  int shape = test_hook(kHookMxKernel);
+  if (shape < 0) shape = count_tiles(g, 256, a_format == kMxFp4 ? 256 : 128) >= 256 ? 0 : count_tiles(g, 128, 128) >= 256 ? 1 : 2;
+  return a_format == kMxFp4 ? launch_shape<kMxFp4>(g, shape, st) : launch_shape<kMxFp8>(g, shape, st);
 }
 
 }  // namespace hago
