@@ -2,9 +2,9 @@
 //
 // D[i][j] = sum_k P[i][k] Q[j][k], P = weights (i = feature, contiguous in the result), Q = activations.  A stage is 256 k of a tile's
 // rows: 128 bytes of a row of 4-bit codes (whole lines), two planes of 128 bytes of one of 8-bit codes, and 8 scale bytes a row.
-// Two slots of LDS hold a stage each.  A stage has four groups of 64 k, one matrix instruction per 32 x 32 block each; fragments
+// SLOTS slots of LDS hold a stage each.  A stage has four groups of 64 k, one matrix instruction per 32 x 32 block each; fragments
 // are double-buffered by groups, so that before its last group a stage has been read completely: there lies the one barrier of a stage,
-// behind it the loads of the stage after next go out into the slot just read, and the next group's fragments come from the other slot.
+// behind it the loads of a later stage go out into the slot just read, and the next group's fragments come from the next slot.
 //
 // LDS.  A load of a wavefront fills 1 KB: 8 rows of 128 bytes, the 16-byte chunks of a row permuted by bits 1 to 3 of the row
 // (swz in qgemm_stream.h), on the global side, so that fragments are read at the full rate.  Scales lie as [row][8 bytes]; a lane takes both dwords of its row and shifts
@@ -28,23 +28,23 @@ __device__ __forceinline__ void mx_dma4(v4i rsrc, uint32_t lds_addr, uint32_t vo
                : "memory", "m0");
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
 struct MxTile {
   static constexpr int NW = WP * WQ, NT = 64 * NW;
   static constexpr int BP = WP * TP * 32, BQ = WQ * TQ * 32;
   static constexpr int PLANES = FA == kMxFp8 ? 2 : 1;
   static constexpr int DATA = (BP + PLANES * BQ) * 128, STAGE = DATA + (BP + BQ) * 8;
   static constexpr int PITCH = TP * 128 + 16;  // bytes of a result row in LDS, at most
-  static constexpr int LDS = 2 * STAGE > NW * 32 * PITCH ? 2 * STAGE : NW * 32 * PITCH;
+  static constexpr int LDS = SLOTS * STAGE > NW * 32 * PITCH ? SLOTS * STAGE : NW * 32 * PITCH;
 };
 
-template <int FA, int WP, int WQ, int TP, int TQ>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
 __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) {
-  using Tile = MxTile<FA, WP, WQ, TP, TQ>;
+  using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS>;
   constexpr int NW = Tile::NW, BP = Tile::BP, BQ = Tile::BQ, PLANES = Tile::PLANES, DATA = Tile::DATA, STAGE = Tile::STAGE;
   constexpr int GP = BP / 8, G = GP + PLANES * BQ / 8;   // loads of a stage: of P, in all
   constexpr int L = G / NW;                              // a wavefront issues loads wave, wave + NW, ...
-  static_assert(GP % NW == 0 && G % NW == 0, "a load's operand is the same in every wavefront");
+  static_assert(GP % NW == 0 && G % NW == 0 && NW % 2 == 0, "a load's operand is the same in every wavefront");
   constexpr int GS = (BP + BQ) / 32, LS = (GS + NW - 1) / NW;  // loads of scales (some twice where NW does not divide them)
   constexpr int NM = TP * TQ;
 
@@ -80,7 +80,6 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
 
   // the lane's byte offset of every load: its row's start and its chunk of a stage (the chunk is the same in every load, since
   // every load of a wavefront has the wavefront's parity)
-  static_assert(NW % 2 == 0, "");
   const int lrow = lane / 8;
   const uint32_t lck = (uint32_t)(((lane % 8) ^ swz<128>((wave & 1) * 8 + lrow)) * 16);
   uint32_t voff[L];
@@ -107,6 +106,26 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
     soff[d] = r >= 0 ? (uint32_t)r * sbytes + (uint32_t)(lane % 2) * 4 : kOob;
     sdst[d] = lds0 + (uint32_t)(DATA + grp * 256);
   }
+  // the sums start from the bias (of features beyond the last one, which nobody stores: the last one's)
+  mx_v16f acc[TP][TQ];
+  if (g.bias) {
+    const float* bias = g.bias + (int64_t)rows.expert * g.N;
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float b = bias[min(p0 + (wp * TP + i) * 32 + 8 * (r / 4) + 4 * half + r % 4, g.N - 1)];
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) acc[i][j][r] = b;
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+      for (int j = 0; j < TQ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+  }
   const int KT = (padded + 255) / 256;
   constexpr int ISSUES = L + LS;
   // loads lo .. hi - 1 of a stage
@@ -131,17 +150,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   };
   static_assert(PLANES == 1 || (BQ / 8) % NW == 0, "a load's plane is the same in every wavefront");
   template_int<0> i0;
-  template_int<1> i1;
-  issue(0, i0, i0, template_int<ISSUES>{});
-  issue(1, i1, i0, template_int<ISSUES>{});
-
-  mx_v16f acc[TP][TQ];
-#pragma unroll
-  for (int i = 0; i < TP; ++i)
-#pragma unroll
-    for (int j = 0; j < TQ; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+  [&]<int... I>(std::integer_sequence<int, I...>) { (issue(I, template_int<I>{}, i0, template_int<ISSUES>{}), ...); }(std::make_integer_sequence<int, SLOTS>{});
 
   // fragment addresses inside a stage
   const int frow = lane & 31;
@@ -182,7 +191,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   // Group H of a stage in slot R: multiply its set of fragments, behind the instructions go the reads of the next group's set (from `next`) and,
   // in the last group, of the next stage's scales, and the loads of stage `dma_stage`.
   auto multiply = [&](auto hconst, auto ring, const uint8_t* next, int dma_stage) {
-    constexpr int H = decltype(hconst)::value, S = H & 1, R = decltype(ring)::value;
+    constexpr int H = decltype(hconst)::value, S = H & 1, R = decltype(ring)::value & 1;
     constexpr int reads = NR + (H == 3 ? TP + TQ : 0), each = (reads + NM - 1) / NM > 2 ? (reads + NM - 1) / NM : 2;
     [&]<int... Mi>(std::integer_sequence<int, Mi...>) {
       ([&] {
@@ -209,26 +218,30 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   auto stage_body = [&](int kt, auto ring) {
     constexpr int R = decltype(ring)::value;
     const uint8_t* here = smem + R * STAGE;
-    const uint8_t* other = smem + (R ^ 1) * STAGE;
+    const uint8_t* other = smem + (R + 1) % SLOTS * STAGE;
     multiply(template_int<0>{}, ring, here, 0);
     multiply(template_int<1>{}, ring, here, 0);
     multiply(template_int<2>{}, ring, here, 0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * ISSUES) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    multiply(template_int<3>{}, ring, other, kt + 2);
+    multiply(template_int<3>{}, ring, other, kt + SLOTS);
   };
 
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ISSUES) : "memory");  // stage 0
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * ISSUES) : "memory");  // stage 0
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < NR; ++r) read(smem, i0, i0, r);
 #pragma unroll
   for (int r = 0; r < TP + TQ; ++r) read_scale(smem, i0, r);
   shift_scales(i0);
-  for (int kt = 0; kt < KT; kt += 2) {
-    stage_body(kt, i0);
-    if (kt + 1 < KT) stage_body(kt + 1, i1);
+  static_assert(SLOTS % 2 == 0 && SLOTS * ISSUES <= 63, "sets of scales by the slot's parity; loads that can be counted");
+  for (int kt = 0; kt < KT; kt += SLOTS) {
+    [&]<int... I>(std::integer_sequence<int, I...>) {
+      ([&] {
+        if (I == 0 || kt + I < KT) stage_body(kt + I, template_int<I>{});
+      }(), ...);
+    }(std::make_integer_sequence<int, SLOTS>{});
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the stages beyond K; before LDS is reused)
   __syncthreads();
@@ -248,31 +261,23 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
           const int n = i * 32 + 2 * r + 4 * half;
           T v[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float f = acc[i][j][r + k];
-            if (g.bias) f += n0 + n + k < g.N ? g.bias[(int64_t)rows.expert * g.N + n0 + n + k] : 0.0f;
-            v[k] = (T)f;
-          }
+          for (int k = 0; k < 4; ++k) v[k] = (T)acc[i][j][r + k];
           __builtin_memcpy(mine + frow * kPitch + n * sizeof(T), v, sizeof(v));
         }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       const int q = wq * TQ * 32 + j * 32;
-#pragma unroll
+#pragma unroll 4
       for (int it = 0; it < kLanes / 2; ++it) {
-        const int r = (lane + 64 * it) / kLanes, c = (lane + 64 * it) % kLanes;
-        if (q + r >= nq) continue;
-        const mx_u4 v = *reinterpret_cast<const mx_u4*>(mine + r * kPitch + c * 16);
-        const int n = n0 + c * kVec;
+        const int r = (lane + 64 * it) / kLanes, c = (lane + 64 * it) % kLanes, n = n0 + c * kVec;
+        if (q + r >= nq || n >= g.N) continue;
+        const uint8_t* src = mine + r * kPitch + c * 16;
         T* dst = static_cast<T*>(g.out) + (int64_t)(rows.row + q + r) * g.N + n;
         if (n + kVec <= g.N) {
-          *reinterpret_cast<mx_u4_any*>(dst) = v;
+          __builtin_nontemporal_store(*reinterpret_cast<const mx_u4*>(src), reinterpret_cast<mx_u4_any*>(dst));
         } else {
-          T e[kVec];
-          __builtin_memcpy(e, &v, 16);
-#pragma unroll
-          for (int k = 0; k < kVec; ++k)
-            if (n + k < g.N) dst[k] = e[k];
+#pragma unroll 1
+          for (int k = 0; n + k < g.N; ++k) dst[k] = reinterpret_cast<const T*>(src)[k];
         }
       }
       __builtin_amdgcn_wave_barrier();
@@ -283,10 +288,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   else leave.template operator()<kMxF16>();
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
 hipError_t launch_tile(const MxGemmArgs& g, hipStream_t st) {
-  using Tile = MxTile<FA, WP, WQ, TP, TQ>;
-  const auto kern = mx_tile_kernel<FA, WP, WQ, TP, TQ>;
+  using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS>;
+  const auto kern = mx_tile_kernel<FA, WP, WQ, TP, TQ, SLOTS>;
   static std::atomic<uint64_t> attr_set{0};  // the devices whose dynamic-LDS limit is raised
   const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), Tile::LDS, attr_set);
   if (e != hipSuccess) return e;
