@@ -22,8 +22,9 @@ __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(MxGemmArgs g
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int tiles_p = (g.N + BP - 1) / BP;
   const int tile_q = (int)(blockIdx.x / (uint32_t)tiles_p), p0 = (int)(blockIdx.x % (uint32_t)tiles_p) * BP;
-  MxRows rows;
-  if (!mx_find_rows<BQ>(g, [&](int) { return tile_q; }, rows)) return;
+  const MxGroups<BQ> groups(g);
+  if (tile_q >= groups.tiles) return;
+  const MxRows rows = groups.rows(g, tile_q);
   const int nq = min(rows.end - rows.row, BQ);
   const int padded = (g.K + 127) & ~127, steps = padded / 128;
   const int wbytes = padded / 2, abytes = FA == kMxFp4 ? wbytes : padded, sbytes = padded / 32;

@@ -43,31 +43,37 @@ __device__ __forceinline__ MxScan mx_scan(const int32_t* offsets, int T, int exp
   return s;
 }
 
-// Tile `pick(number of tiles)` of the groups' rows; false: pick gave none (a negative number, or one beyond them).  pick is called once, with a uniform number.
-template <int ROWS, typename Pick>
-__device__ __forceinline__ bool mx_find_rows(const MxGemmArgs& g, const Pick& pick, MxRows& rows) {
-  if (!g.offsets) {
-    const int tile = pick((int)((uint32_t)(g.T + ROWS - 1) / ROWS));
-    rows = {0, tile * ROWS, g.T};
-    return tile >= 0 && rows.row < g.T;
+// The tiles of all groups, found by their numbers.  Up to 64 groups stay in registers, one a lane; of more the array is gone
+// through again for every tile.
+template <int ROWS>
+struct MxGroups {
+  MxScan first;
+  int tiles;
+  __device__ __forceinline__ explicit MxGroups(const MxGemmArgs& g) {
+    if (!g.offsets) {
+      first = {0, 0, 0, 0};
+      tiles = (int)((uint32_t)(g.T + ROWS - 1) / ROWS);
+      return;
+    }
+    first = mx_scan<ROWS>(g.offsets, g.T, g.experts, 0, 0);
+    tiles = __builtin_amdgcn_readlane(first.upto, 63);
+    for (int e = 64; e < g.experts; e += 64) tiles = __builtin_amdgcn_readlane(mx_scan<ROWS>(g.offsets, g.T, g.experts, e, tiles).upto, 63);
   }
-  auto last = [](int v) { return __builtin_amdgcn_readlane(v, 63); };
-  MxScan s = mx_scan<ROWS>(g.offsets, g.T, g.experts, 0, 0);
-  int total = last(s.upto);
-  for (int first = 64; first < g.experts; first += 64) total = last(mx_scan<ROWS>(g.offsets, g.T, g.experts, first, total).upto);
-  const int tile = pick(total);
-  if (tile < 0 || tile >= total) return false;
-  for (int first = 0;; first += 64) {
-    if (first) s = mx_scan<ROWS>(g.offsets, g.T, g.experts, first, last(s.upto));
-    const uint64_t there = __ballot(tile < s.upto);
-    if (there) {
-      const int l = __builtin_ctzll(there);
-      const int lo = __builtin_amdgcn_readlane(s.lo, l), upto = __builtin_amdgcn_readlane(s.upto, l), here = __builtin_amdgcn_readlane(s.here, l);
-      rows = {first + l, lo + (tile - (upto - here)) * ROWS, __builtin_amdgcn_readlane(s.hi, l)};
-      return true;
+  // tile: uniform, below `tiles`
+  __device__ __forceinline__ MxRows rows(const MxGemmArgs& g, int tile) const {
+    if (!g.offsets) return {0, tile * ROWS, g.T};
+    MxScan s = first;
+    for (int e = 0;; e += 64) {
+      if (e) s = mx_scan<ROWS>(g.offsets, g.T, g.experts, e, __builtin_amdgcn_readlane(s.upto, 63));
+      const uint64_t there = __ballot(tile < s.upto);
+      if (there) {
+        const int l = __builtin_ctzll(there);
+        const int lo = __builtin_amdgcn_readlane(s.lo, l), upto = __builtin_amdgcn_readlane(s.upto, l), here = __builtin_amdgcn_readlane(s.here, l);
+        return {e + l, lo + (tile - (upto - here)) * ROWS, __builtin_amdgcn_readlane(s.hi, l)};
+      }
     }
   }
-}
+};
 
 // The row of A that result row t is made of.
 __device__ __forceinline__ int mx_row_of(const MxGemmArgs& g, int t) {

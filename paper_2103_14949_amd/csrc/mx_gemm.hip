@@ -26,14 +26,14 @@ struct MxShape {
 };
 constexpr int kShapes = 11;
 constexpr MxShape kMxShapes[2][kShapes] = {
-    {{256, 256, 0, 0.00f, 6.32f, 0.30f, 1.24f, 0}, {128, 128, 0, 2.46f, 2.17f, 0.66f, 0.54f, 0}, {128, 64, 0, 2.83f, 1.04f, 0.47f, 0.43f, 0},
-     {64, 64, 0, 2.85f, 0.58f, 0.34f, 0.28f, 0}, {64, 32, 0, 2.90f, 0.77f, 0.28f, 0.21f, 0},
-     {16, 16, 4, 2.59f, 0.11f, 0.32f, 0.195f, 0.013f}, {16, 16, 8, 2.49f, 0.33f, 0.27f, 0.185f, 0.0f}, {32, 16, 2, 2.99f, 0.0f, 0.09f, 0.366f, 0.041f},
-     {32, 16, 4, 2.65f, 0.23f, 0.22f, 0.307f, 0.044f}, {32, 16, 8, 2.32f, 0.58f, 0.88f, 0.301f, 0.010f}, {32, 32, 16, 1.04f, 3.07f, 2.69f, 0.174f, 0.092f}},
-    {{256, 128, 0, 0.00f, 4.91f, 1.00f, 1.28f, 0}, {128, 128, 0, 0.22f, 4.78f, 0.55f, 0.82f, 0}, {128, 64, 0, 2.63f, 1.42f, 0.65f, 0.55f, 0},
-     {64, 64, 0, 2.80f, 0.80f, 0.47f, 0.34f, 0}, {64, 32, 0, 2.75f, 1.21f, 0.34f, 0.27f, 0},
-     {16, 16, 4, 2.65f, 0.02f, 0.29f, 0.240f, 0.096f}, {16, 16, 8, 2.55f, 0.23f, 0.50f, 0.228f, 0.090f}, {32, 16, 2, 3.00f, 0.0f, 0.30f, 0.383f, 0.119f},
-     {32, 16, 4, 2.75f, 0.15f, 0.38f, 0.372f, 0.094f}, {32, 16, 8, 2.39f, 0.48f, 0.56f, 0.361f, 0.064f}, {32, 32, 16, 0.77f, 3.05f, 3.54f, 0.315f, 0.134f}}};
+    {{256, 256, 0, 0.00f, 6.25f, 0.81f, 1.21f, 0}, {128, 128, 0, 3.65f, 1.73f, 0.63f, 0.56f, 0}, {128, 64, 0, 3.66f, 0.94f, 0.53f, 0.42f, 0},
+     {64, 64, 0, 2.72f, 0.56f, 0.33f, 0.28f, 0}, {64, 32, 0, 2.86f, 0.75f, 0.29f, 0.21f, 0},
+     {16, 16, 4, 2.615f, 0.100f, 0.343f, 0.195f, 0.017f}, {16, 16, 8, 2.527f, 0.303f, 0.553f, 0.184f, 0.007f}, {32, 16, 2, 3.148f, 0.000f, 0.295f, 0.366f, 0.029f},
+     {32, 16, 4, 2.807f, 0.195f, 0.271f, 0.294f, 0.049f}, {32, 16, 8, 2.392f, 0.607f, 0.776f, 0.291f, 0.015f}, {32, 32, 16, 1.057f, 3.026f, 2.788f, 0.193f, 0.080f}},
+    {{256, 128, 0, 0.33f, 5.60f, 0.93f, 1.23f, 0}, {128, 128, 0, 1.73f, 3.93f, 0.87f, 0.82f, 0}, {128, 64, 0, 3.58f, 1.19f, 0.69f, 0.51f, 0},
+     {64, 64, 0, 2.65f, 0.75f, 0.47f, 0.34f, 0}, {64, 32, 0, 2.61f, 1.16f, 0.39f, 0.27f, 0},
+     {16, 16, 4, 2.666f, 0.028f, 0.336f, 0.237f, 0.095f}, {16, 16, 8, 2.572f, 0.251f, 0.577f, 0.218f, 0.095f}, {32, 16, 2, 3.063f, 0.000f, 0.300f, 0.390f, 0.104f},
+     {32, 16, 4, 2.891f, 0.136f, 0.478f, 0.338f, 0.112f}, {32, 16, 8, 2.484f, 0.559f, 0.333f, 0.335f, 0.073f}, {32, 32, 16, 0.769f, 3.041f, 3.558f, 0.301f, 0.144f}}};
 
 int pick_shape(const MxGemmArgs& g, int a_format) {
   const double k = (double)mx_padded(g.K);

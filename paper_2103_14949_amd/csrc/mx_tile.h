@@ -7,8 +7,8 @@
 // behind it the loads of a later stage go out into the slot just read, and the next group's fragments come from the next slot.
 //
 // LDS.  A load of a wavefront fills 1 KB: 8 rows of 128 bytes, the 16-byte chunks of a row permuted by bits 1 to 3 of the row
-// (swz in qgemm_stream.h), on the global side, so that fragments are read at the full rate.  Scales lie as [row][8 bytes]; a lane takes both dwords of its row and shifts
-// its half's byte of either pair down, so that one instruction's byte select serves both halves of the wavefront.
+// (swz in qgemm_stream.h), on the global side, so that fragments are read at the full rate.  Scales lie as [row][8 bytes]; a lane takes a dword for half a stage and shifts
+// its half's byte of either pair down, so that one byte select serves both halves of the wavefront.
 //
 // Out of range.  Loads go through descriptors of the tile's own rows (64-bit base, so tensors have any size), and lanes whose row or k
 // lies outside get an offset beyond: zeros, code and scale, whose products are zero.
@@ -21,11 +21,21 @@ namespace hago {
 
 namespace {
 
-__device__ __forceinline__ void mx_dma4(v4i rsrc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+// Loads into the LDS (qgemm_stream.h) at a constant distance behind a scalar address: what lies in scalar registers for every load of every
+// slot is missing elsewhere.
+template <int AT>
+__device__ __forceinline__ void mx_dma16(v4i rsrc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
-               : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff)
-               : "memory", "m0");
+               : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff), "n"(AT)
+               : "memory", "m0", "scc");
+}
+template <int AT>
+__device__ __forceinline__ void mx_dma4(v4i rsrc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :
+               : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff), "n"(AT)
+               : "memory", "m0", "scc");
 }
 
 template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
@@ -34,9 +44,105 @@ struct MxTile {
   static constexpr int BP = WP * TP * 32, BQ = WQ * TQ * 32;
   static constexpr int PLANES = FA == kMxFp8 ? 2 : 1;
   static constexpr int DATA = (BP + PLANES * BQ) * 128, STAGE = DATA + (BP + BQ) * 8;
+  // rows leave from the registers where a wavefront has pairs of 32-feature blocks, by LDS otherwise
+  static constexpr bool BY_LDS = TP % 2 != 0;
   static constexpr int PITCH = TP * 128 + 16;  // bytes of a result row in LDS, at most
-  static constexpr int LDS = SLOTS * STAGE > NW * 32 * PITCH ? SLOTS * STAGE : NW * 32 * PITCH;
+  static constexpr int LDS = !BY_LDS || SLOTS * STAGE > NW * 32 * PITCH ? SLOTS * STAGE : NW * 32 * PITCH;
+  // A workgroup goes from tile to tile; the next one's first stages are under way while a tile's results leave.
+  static constexpr bool STAYS = !BY_LDS && SLOTS == 2 && TP * TQ < 8;
+  static constexpr bool EARLY = TP * TQ < 8;  // its rows are looked up a tile ahead, where registers allow
+  static constexpr int RESIDENT = 160 * 1024 / LDS < 16 / NW ? 160 * 1024 / LDS : 16 / NW;  // workgroups that a CU holds
 };
+
+// 32 rows of a wavefront's features at a time go through its own piece of LDS and leave by whole rows.
+template <int TYPE, int TP, int TQ>
+__device__ __forceinline__ void leave_by_lds(const MxGemmArgs& g, const mx_v16f (&acc)[TP][TQ], int row, int q0, int nq, int n0, int lane, uint8_t* mine) {
+  using T = typename MxElement<TYPE>::type;
+  constexpr int kPitch = TP * 32 * sizeof(T) + 16, kVec = 16 / sizeof(T), kLanes = TP * 32 / kVec;
+  const int half = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < TQ; ++j) {
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        T v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (T)acc[i][j][r + k];
+        __builtin_memcpy(mine + (lane & 31) * kPitch + (i * 32 + 2 * r + 4 * half) * sizeof(T), v, sizeof(v));
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+    for (int it = 0; it < kLanes / 2; ++it) {
+      const int r = q0 + j * 32 + (lane + 64 * it) / kLanes, c = (lane + 64 * it) % kLanes, n = n0 + c * kVec;
+      if (r >= nq || n >= g.N) continue;
+      const uint8_t* src = mine + (lane + 64 * it) / kLanes * kPitch + c * 16;
+      T* dst = static_cast<T*>(g.out) + (int64_t)(row + r) * g.N + n;
+      if (n + kVec <= g.N) {
+        __builtin_nontemporal_store(*reinterpret_cast<const mx_u4*>(src), reinterpret_cast<mx_u4_any*>(dst));
+      } else {
+#pragma unroll 1
+        for (int k = 0; n + k < g.N; ++k) dst[k] = reinterpret_cast<const T*>(src)[k];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Straight from the registers.  A lane has 4 features in every 8 of its row; the halves of the wavefront exchange theirs between two blocks of 32
+// features, so that either has whole rows of one, and the lanes of a quad exchange 16-byte pieces, so that a quad stores 64
+// consecutive bytes of a row at a time.
+template <int TYPE, int TP, int TQ>
+__device__ __forceinline__ void leave_by_quads(const MxGemmArgs& g, const mx_v16f (&acc)[TP][TQ], int row, int q0, int nq, int n0, int lane) {
+  using T = typename MxElement<TYPE>::type;
+  constexpr int kVec = 16 / sizeof(T), D = sizeof(T), kSets = sizeof(T) / 2;  // dwords of 4 features / 2, sets of 64 bytes in 32 features
+  const int half = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < TQ; ++j)
+#pragma unroll
+    for (int i = 0; i < TP; i += 2) {
+      uint32_t piece[4 * kSets][4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        T a[4], b[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = (T)acc[i][j][4 * q + k], b[k] = (T)acc[i + 1][j][4 * q + k];
+        uint32_t x[D], y[D];
+        __builtin_memcpy(x, a, sizeof(a));
+        __builtin_memcpy(y, b, sizeof(b));
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+          const auto s = __builtin_amdgcn_permlane32_swap(x[d], y[d], false, false);
+          // (this lane's block: features 8 q + 0 .. 3 and 8 q + 4 .. 7)
+          if constexpr (D == 2) piece[q][d] = s[0], piece[q][2 + d] = s[1];
+          else piece[2 * q][d] = s[0], piece[2 * q + 1][d] = s[1];
+        }
+      }
+#pragma unroll
+      for (int set = 0; set < kSets; ++set) {
+        uint32_t(&p)[4][4] = *reinterpret_cast<uint32_t(*)[4][4]>(&piece[4 * set]);
+        quad_transpose<4>(p, lane);
+        const int n = n0 + (i + half) * 32 + set * 4 * kVec + (lane & 3) * kVec;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int r = q0 + j * 32 + (lane & 28) + t;
+          if (r >= nq || n >= g.N) continue;
+          T* dst = static_cast<T*>(g.out) + (int64_t)(row + r) * g.N + n;
+          const mx_u4 v = {p[t][0], p[t][1], p[t][2], p[t][3]};
+          if (n + kVec <= g.N) {
+            __builtin_nontemporal_store(v, reinterpret_cast<mx_u4_any*>(dst));
+          } else {
+            T e[kVec];
+            __builtin_memcpy(e, &v, 16);
+#pragma unroll
+            for (int k = 0; k < kVec - 1; ++k)
+              if (n + k < g.N) dst[k] = e[k];
+          }
+        }
+      }
+    }
+}
 
 template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
 __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) {
@@ -53,80 +159,73 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wp = wave % WP, wq = wave / WP;
 
-  const int tiles_p = (g.N + BP - 1) / BP;
-  int tile_p = 0;
-  MxRows rows;
-  const bool any = mx_find_rows<BQ>(g, [&](int tiles_q) {
-    const uint32_t count = (uint32_t)tiles_p * (uint32_t)tiles_q;
-    if (blockIdx.x >= count) return -1;
-    int tile_q;
-    panel_tile((int)xcd_run(blockIdx.x, count), tiles_p, tiles_q, tile_p, tile_q);
-    return tile_q;
-  }, rows);
-  if (!any) return;
-  const int p0 = tile_p * BP;
-  const int np = min(g.N - p0, BP), nq = min(rows.end - rows.row, BQ);
-
   const int padded = (g.K + 127) & ~127;
   const uint32_t wbytes = (uint32_t)padded / 2, abytes = FA == kMxFp4 ? wbytes : (uint32_t)padded, sbytes = (uint32_t)padded / 32;
-  const int64_t wrow = (int64_t)rows.expert * g.N + p0, arow = g.index ? 0 : rows.row;
-  const uint32_t arows = g.index ? (uint32_t)g.a_rows : (uint32_t)nq;
-  const v4i rs_w = make_rsrc(g.w + wrow * wbytes, (uint32_t)np * wbytes), rs_ws = make_rsrc(g.w_scale + wrow * sbytes, (uint32_t)np * sbytes);
-  const v4i rs_a = make_rsrc(g.a + arow * abytes, arows * abytes), rs_as = make_rsrc(g.a_scale + arow * sbytes, arows * sbytes);
-  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem;
+  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem, wave_lds = lds0 + (uint32_t)wave * 1024;
+  // (of a workgroup that stays, whole rounds of the slots: its last stage may hold nothing)
+  const int KT = (padded + 255) / 256, stages = Tile::STAYS ? (KT + SLOTS - 1) / SLOTS * SLOTS : KT;
 
-  // row r of the tile's activations -> its row among those the descriptors begin with; negative: none
-  auto a_row = [&](int r) { return r < nq ? (g.index ? mx_row_of(g, rows.row + r) : r) : -1; };
+  const int tiles_p = (g.N + BP - 1) / BP;
+  const MxGroups<BQ> groups(g);
+  const uint32_t count = (uint32_t)tiles_p * (uint32_t)groups.tiles;
+  uint32_t id = blockIdx.x;
+  if (id >= count) return;
+  struct Place {
+    MxRows rows;
+    int p0;
+  };
+  auto place_of = [&](uint32_t id) {
+    int tile_p, tile_q;
+    panel_tile((int)xcd_run(id, count), tiles_p, groups.tiles, tile_p, tile_q);
+    return Place{groups.rows(g, tile_q), tile_p * BP};
+  };
 
-  // the lane's byte offset of every load: its row's start and its chunk of a stage (the chunk is the same in every load, since
-  // every load of a wavefront has the wavefront's parity)
+  // The rows of a tile's activations that this lane loads, of those the descriptors begin with; negative: none.  Both planes of a row are the same
+  // lane's, so one of PLANES loads stands for all.
+  constexpr int LQ = (G - GP) / NW / PLANES;
   const int lrow = lane / 8;
-  const uint32_t lck = (uint32_t)(((lane % 8) ^ swz<128>((wave & 1) * 8 + lrow)) * 16);
-  uint32_t voff[L];
+  struct Picked {
+    int q[LQ], s[LS];
+  };
+  auto pick_rows = [&](const Place& at) {
+    const int nq = min(at.rows.end - at.rows.row, BQ);
+    auto row_of = [&](int r) { return r < nq ? (g.index ? mx_row_of(g, at.rows.row + r) : r) : -1; };
+    Picked p;
 #pragma unroll
-  for (int d = 0; d < L; ++d) {
-    const bool isq = d >= GP / NW;
-    if (!isq) {
-      const int r = (wave + NW * d) * 8 + lrow;
-      voff[d] = r < np ? (uint32_t)r * wbytes + lck : kOob;
-    } else {
-      const int v = (wave + NW * d - GP) * 8 + lrow, r = a_row(v % BQ);
-      voff[d] = r >= 0 ? (uint32_t)r * abytes + lck + (uint32_t)(v / BQ) * 128 : kOob;
+    for (int d = 0; d < LQ; ++d) p.q[d] = row_of((wave + NW * d) * 8 + lrow);
+#pragma unroll
+    for (int d = 0; d < LS; ++d) {
+      const int v = (wave + NW * d) % GS * 32 + lane / 2;
+      p.s[d] = v >= BP ? row_of(v - BP) : at.p0 + v < g.N ? v : -1;
     }
-  }
-  uint32_t soff[LS];
-  uint32_t sdst[LS];
-  bool sisq[LS];
+    return p;
+  };
+
+  // A tile's descriptors, and the lane's byte offset of every load: its row's start and its chunk of a stage (the chunk is the same in
+  // every load, since every load of a wavefront has the wavefront's parity).
+  const uint32_t lck = (uint32_t)(((lane % 8) ^ swz<128>((wave & 1) * 8 + lrow)) * 16);
+  v4i rs_w, rs_ws, rs_a, rs_as;
+  uint32_t voff[L], soff[LS];
+  auto bind = [&](const Place& at, const Picked& picked) {
+    const int np = min(g.N - at.p0, BP), nq = min(at.rows.end - at.rows.row, BQ);
+    const int64_t wrow = (int64_t)at.rows.expert * g.N + at.p0, arow = g.index ? 0 : at.rows.row;
+    const uint32_t arows = g.index ? (uint32_t)g.a_rows : (uint32_t)nq;
+    rs_w = make_rsrc(g.w + wrow * wbytes, (uint32_t)np * wbytes), rs_ws = make_rsrc(g.w_scale + wrow * sbytes, (uint32_t)np * sbytes);
+    rs_a = make_rsrc(g.a + arow * abytes, arows * abytes), rs_as = make_rsrc(g.a_scale + arow * sbytes, arows * sbytes);
 #pragma unroll
-  for (int d = 0; d < LS; ++d) {
-    const int grp = (wave + NW * d) % GS;
-    const int v = grp * 32 + lane / 2;
-    sisq[d] = grp >= BP / 32;
-    const int r = sisq[d] ? a_row(v - BP) : v < np ? v : -1;
-    soff[d] = r >= 0 ? (uint32_t)r * sbytes + (uint32_t)(lane % 2) * 4 : kOob;
-    sdst[d] = lds0 + (uint32_t)(DATA + grp * 256);
-  }
-  // the sums start from the bias (of features beyond the last one, which nobody stores: the last one's)
-  mx_v16f acc[TP][TQ];
-  if (g.bias) {
-    const float* bias = g.bias + (int64_t)rows.expert * g.N;
-#pragma unroll
-    for (int i = 0; i < TP; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float b = bias[min(p0 + (wp * TP + i) * 32 + 8 * (r / 4) + 4 * half + r % 4, g.N - 1)];
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) acc[i][j][r] = b;
+    for (int d = 0; d < L; ++d) {
+      if (d < GP / NW) {
+        const int r = (wave + NW * d) * 8 + lrow;
+        voff[d] = r < np ? (uint32_t)r * wbytes + lck : kOob;
+      } else {
+        constexpr int kPlane = PLANES == 1 ? 0 : LQ;  // loads of a plane
+        const int e = d - GP / NW, plane = kPlane ? e / kPlane : 0, r = picked.q[kPlane ? e % kPlane : e];
+        voff[d] = r >= 0 ? (uint32_t)r * abytes + lck + (uint32_t)plane * 128 : kOob;
       }
-  } else {
+    }
 #pragma unroll
-    for (int i = 0; i < TP; ++i)
-#pragma unroll
-      for (int j = 0; j < TQ; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-  }
-  const int KT = (padded + 255) / 256;
+    for (int d = 0; d < LS; ++d) soff[d] = picked.s[d] >= 0 ? (uint32_t)picked.s[d] * sbytes + (uint32_t)(lane % 2) * 4 : kOob;
+  };
   constexpr int ISSUES = L + LS;
   // loads lo .. hi - 1 of a stage
   auto issue = [&](int stage, auto slot, auto lo, auto hi) {
@@ -138,20 +237,21 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
         constexpr int d = decltype(lo)::value + I;
         if constexpr (d < L) {
           constexpr bool isq = d >= GP / NW;
-          constexpr int plane = isq ? ((NW * d - GP) * 8) / BQ : 0;  // (BQ rows are whole rounds of loads, or all of a round)
+          constexpr int plane = isq && PLANES > 1 ? (d - GP / NW) / LQ : 0;
           const uint32_t at = (isq ? kq + plane * 128 : kp) + lck, end = isq ? abytes : wbytes;
-          dma16s(isq ? rs_a : rs_w, lds0 + (uint32_t)(base + NW * d * 1024) + (uint32_t)wave * 1024, at < end ? voff[d] : kOob, there ? (isq ? kq : kp) : 0);
+          mx_dma16<base + NW * d * 1024>(isq ? rs_a : rs_w, wave_lds, at < end ? voff[d] : kOob, there ? (isq ? kq : kp) : 0);
         } else {
           constexpr int s = d - L;
-          mx_dma4(sisq[s] ? rs_as : rs_ws, sdst[s] + base, ks + (uint32_t)(lane % 2) * 4 < sbytes ? soff[s] : kOob, there ? ks : 0);
+          const int grp = (wave + NW * s) % GS;
+          mx_dma4<base + DATA>(grp >= BP / 32 ? rs_as : rs_ws, lds0 + (uint32_t)grp * 256, ks + (uint32_t)(lane % 2) * 4 < sbytes ? soff[s] : kOob, there ? ks : 0);
         }
       }(), ...);
     }(std::make_integer_sequence<int, decltype(hi)::value - decltype(lo)::value>{});
   };
   static_assert(PLANES == 1 || (BQ / 8) % NW == 0, "a load's plane is the same in every wavefront");
   template_int<0> i0;
-  [&]<int... I>(std::integer_sequence<int, I...>) { (issue(I, template_int<I>{}, i0, template_int<ISSUES>{}), ...); }(std::make_integer_sequence<int, SLOTS>{});
 
+  mx_v16f acc[TP][TQ];
   // fragment addresses inside a stage
   const int frow = lane & 31;
   auto chunk_at = [&](int c) { return (c ^ swz<128>(frow & 15)) * 16; };
@@ -169,9 +269,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   }
   const int psa = DATA + prow * 8, qsa = DATA + (BP + qrow) * 8, shift = 8 * half;
   constexpr int kFrag = 32 * 128;
-  typedef uint32_t v2u __attribute__((ext_vector_type(2)));
   mx_v4i pf[2][TP], qf[2][TQ * PLANES];
-  v2u sc[2][TP + TQ];
+  uint32_t sc[2][TP + TQ];  // scales of the first and of the second half of a stage
   // read r of the NR of a group's operands, activations first
   constexpr int NR = TQ * PLANES + TP;
   auto read = [&](const uint8_t* base, auto set, auto group, int r) {
@@ -179,20 +278,20 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
     if (r < TQ * PLANES) qf[S][r] = *reinterpret_cast<const mx_v4i*>(base + qa[PLANES * H + r % PLANES] + (r / PLANES) * kFrag);
     else pf[S][r - TQ * PLANES] = *reinterpret_cast<const mx_v4i*>(base + pa[H] + (r - TQ * PLANES) * kFrag);
   };
-  auto read_scale = [&](const uint8_t* base, auto set, int r) {
-    constexpr int S = decltype(set)::value;
-    sc[S][r] = *reinterpret_cast<const v2u*>(base + (r < TP ? psa + r * 256 : qsa + (r - TP) * 256));
+  auto read_scale = [&](const uint8_t* base, auto part, int r) {
+    constexpr int S = decltype(part)::value;
+    sc[S][r] = *reinterpret_cast<const uint32_t*>(base + (r < TP ? psa + r * 256 : qsa + (r - TP) * 256) + 4 * S);
   };
-  auto shift_scales = [&](auto set) {
-    constexpr int S = decltype(set)::value;
+  auto shift_scales = [&](auto part) {
+    constexpr int S = decltype(part)::value;
 #pragma unroll
-    for (int r = 0; r < TP + TQ; ++r) sc[S][r] = sc[S][r] >> (uint32_t)shift;
+    for (int r = 0; r < TP + TQ; ++r) sc[S][r] >>= shift;
   };
-  // Group H of a stage in slot R: multiply its set of fragments, behind the instructions go the reads of the next group's set (from `next`) and,
-  // in the last group, of the next stage's scales, and the loads of stage `dma_stage`.
+  // Group H of a stage: multiply its set of fragments, behind the instructions go the reads of the next group's set (from `next`) and of
+  // the next half's scales in front of it, and in the last group the loads of stage `dma_stage`.
   auto multiply = [&](auto hconst, auto ring, const uint8_t* next, int dma_stage) {
-    constexpr int H = decltype(hconst)::value, S = H & 1, R = decltype(ring)::value & 1;
-    constexpr int reads = NR + (H == 3 ? TP + TQ : 0), each = (reads + NM - 1) / NM > 2 ? (reads + NM - 1) / NM : 2;
+    constexpr int H = decltype(hconst)::value, S = H & 1;
+    constexpr int reads = NR + (H % 2 ? TP + TQ : 0), each = (reads + NM - 1) / NM > 2 ? (reads + NM - 1) / NM : 2;
     [&]<int... Mi>(std::integer_sequence<int, Mi...>) {
       ([&] {
         constexpr int m = Mi, j = m / TP, i = m % TP;
@@ -201,91 +300,117 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
         mx_v8i q;
         if constexpr (FA == kMxFp4) q = __builtin_shufflevector(q4, q4, 0, 1, 2, 3, -1, -1, -1, -1);
         else q = __builtin_shufflevector(q4, q5, 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 2 * (H % 2), (int)sc[R][i][H / 2],
-                                                                    2 * (H % 2), (int)sc[R][TP + j][H / 2]);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 2 * (H % 2), (int)sc[H / 2][i],
+                                                                    2 * (H % 2), (int)sc[H / 2][TP + j]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = each * m; r < each * m + each && r < reads; ++r) {
           if (r < NR) read(next, template_int<(S ^ 1)>{}, template_int<(H + 1) % 4>{}, r);
-          else read_scale(next, template_int<(R ^ 1)>{}, r - NR);
+          else read_scale(next, template_int<(H / 2 ^ 1)>{}, r - NR);
         }
         if constexpr (H == 3) issue(dma_stage, ring, template_int<m * ISSUES / NM>{}, template_int<(m + 1) * ISSUES / NM>{});
         __builtin_amdgcn_sched_barrier(0);
       }(), ...);
     }(std::make_integer_sequence<int, NM>{});
-    if constexpr (H == 3) shift_scales(template_int<(R ^ 1)>{});
+    if constexpr (H % 2 != 0) shift_scales(template_int<(H / 2 ^ 1)>{});
   };
+  constexpr int kStores16 = TQ * TP / 2 * 4, kStores32 = 2 * kStores16;
+  int stores = 0;  // of the last tile's results, behind the loads of this one's first two stages
+  bool first = true, more = false;
   auto stage_body = [&](int kt, auto ring) {
     constexpr int R = decltype(ring)::value;
     const uint8_t* here = smem + R * STAGE;
     const uint8_t* other = smem + (R + 1) % SLOTS * STAGE;
-    multiply(template_int<0>{}, ring, here, 0);
-    multiply(template_int<1>{}, ring, here, 0);
-    multiply(template_int<2>{}, ring, here, 0);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * ISSUES) : "memory");
+    const bool blank = Tile::STAYS && kt >= KT;
+    if (!blank) {
+      multiply(template_int<0>{}, ring, here, 0);
+      multiply(template_int<1>{}, ring, here, 0);
+      multiply(template_int<2>{}, ring, here, 0);
+    }
+    // the next stage has landed; the stores behind it need not have
+    if (Tile::STAYS && kt == 0 && stores == kStores16) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStores16) : "memory");
+    else if (Tile::STAYS && kt == 0 && stores == kStores32) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStores32) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 2) * ISSUES) : "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    multiply(template_int<3>{}, ring, other, kt + SLOTS);
+    // (stages behind the last one are the next tile's)
+    const int fetch = Tile::STAYS && more && kt + SLOTS >= stages ? kt + SLOTS - stages : kt + SLOTS;
+    if (!blank) multiply(template_int<3>{}, ring, other, fetch);
+    else issue(fetch, ring, i0, template_int<ISSUES>{});
+  };
+  auto by_type = [&](const auto& f) {
+    if (g.type == kMxF32) f.template operator()<kMxF32>();
+    else if (g.type == kMxBf16) f.template operator()<kMxBf16>();
+    else f.template operator()<kMxF16>();
   };
 
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * ISSUES) : "memory");  // stage 0
-  __syncthreads();
-#pragma unroll
-  for (int r = 0; r < NR; ++r) read(smem, i0, i0, r);
-#pragma unroll
-  for (int r = 0; r < TP + TQ; ++r) read_scale(smem, i0, r);
-  shift_scales(i0);
-  static_assert(SLOTS % 2 == 0 && SLOTS * ISSUES <= 63, "sets of scales by the slot's parity; loads that can be counted");
-  for (int kt = 0; kt < KT; kt += SLOTS) {
-    [&]<int... I>(std::integer_sequence<int, I...>) {
-      ([&] {
-        if (I == 0 || kt + I < KT) stage_body(kt + I, template_int<I>{});
-      }(), ...);
-    }(std::make_integer_sequence<int, SLOTS>{});
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the stages beyond K; before LDS is reused)
-  __syncthreads();
+  Place here = place_of(id);
+  bind(here, pick_rows(here));
+  [&]<int... I>(std::integer_sequence<int, I...>) { (issue(I, template_int<I>{}, i0, template_int<ISSUES>{}), ...); }(std::make_integer_sequence<int, SLOTS>{});
+  for (;;) {
+    // the next tile's rows are looked up now and used when this one's loads have all gone out
+    more = Tile::STAYS && id + g.grid < count;
+    Place next = here;
+    Picked picked;
+    if (more) next = place_of(id + g.grid);
+    if (more) picked = pick_rows(next);
 
-  // Results: 32 rows of a wavefront's features at a time go through its own piece of LDS and leave by whole rows.
-  uint8_t* mine = smem + wave * 32 * Tile::PITCH;
-  const int n0 = p0 + wp * TP * 32;
-  auto leave = [&]<int TYPE>() {
-    using T = typename MxElement<TYPE>::type;
-    constexpr int kPitch = TP * 32 * sizeof(T) + 16, kVec = 16 / sizeof(T), kLanes = TP * 32 / kVec;
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) {
+    if (g.bias) {
+      const float* bias = g.bias + (int64_t)here.rows.expert * g.N;
 #pragma unroll
       for (int i = 0; i < TP; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const int n = i * 32 + 2 * r + 4 * half;
-          T v[4];
+        for (int r = 0; r < 16; ++r) {
+          const float b = bias[min(here.p0 + (wp * TP + i) * 32 + 8 * (r / 4) + 4 * half + r % 4, g.N - 1)];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = (T)acc[i][j][r + k];
-          __builtin_memcpy(mine + frow * kPitch + n * sizeof(T), v, sizeof(v));
+          for (int j = 0; j < TQ; ++j) acc[i][j][r] = b;
         }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      const int q = wq * TQ * 32 + j * 32;
-#pragma unroll 4
-      for (int it = 0; it < kLanes / 2; ++it) {
-        const int r = (lane + 64 * it) / kLanes, c = (lane + 64 * it) % kLanes, n = n0 + c * kVec;
-        if (q + r >= nq || n >= g.N) continue;
-        const uint8_t* src = mine + r * kPitch + c * 16;
-        T* dst = static_cast<T*>(g.out) + (int64_t)(rows.row + q + r) * g.N + n;
-        if (n + kVec <= g.N) {
-          __builtin_nontemporal_store(*reinterpret_cast<const mx_u4*>(src), reinterpret_cast<mx_u4_any*>(dst));
-        } else {
-#pragma unroll 1
-          for (int k = 0; n + k < g.N; ++k) dst[k] = reinterpret_cast<const T*>(src)[k];
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
+    } else {
+#pragma unroll
+      for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int j = 0; j < TQ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
     }
-  };
-  if (g.type == kMxF32) leave.template operator()<kMxF32>();
-  else if (g.type == kMxBf16) leave.template operator()<kMxBf16>();
-  else leave.template operator()<kMxF16>();
+
+    if (first) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * ISSUES) : "memory");  // stage 0 (of a later tile: waited for in the last stage)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < NR; ++r) read(smem, i0, i0, r);
+#pragma unroll
+    for (int r = 0; r < TP + TQ; ++r) read_scale(smem, i0, r);
+    shift_scales(i0);
+    static_assert(SLOTS * ISSUES <= 63, "loads that can be counted");
+    for (int kt = 0; kt < stages; kt += SLOTS) {
+      if (more && kt + SLOTS >= stages) bind(next, Tile::EARLY ? picked : pick_rows(next));
+      [&]<int... I>(std::integer_sequence<int, I...>) {
+        ([&] {
+          if (I == 0 || Tile::STAYS || kt + I < stages) stage_body(kt + I, template_int<I>{});
+        }(), ...);
+      }(std::make_integer_sequence<int, SLOTS>{});
+    }
+    // The next tile's first stages are on their way into LDS, or in it, while the results leave.
+    const int n0 = here.p0 + wp * TP * 32, nq = min(here.rows.end - here.rows.row, BQ);
+    if constexpr (Tile::BY_LDS) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the stages beyond K; before LDS is used for something else)
+      __syncthreads();
+      uint8_t* mine = smem + wave * 32 * Tile::PITCH;
+      by_type([&]<int TYPE>() { leave_by_lds<TYPE, TP, TQ>(g, acc, here.rows.row, wq * TQ * 32, nq, n0, lane, mine); });
+      return;
+    } else {
+      by_type([&]<int TYPE>() { leave_by_quads<TYPE, TP, TQ>(g, acc, here.rows.row, wq * TQ * 32, nq, n0, lane); });
+      if (!more) break;
+      // (every lane of a whole tile stores, so that the stores can be counted)
+      stores = nq == BQ && n0 + TP * 32 <= g.N ? (g.type == kMxF32 ? kStores32 : kStores16) : 0;
+      first = false;
+      id += g.grid;
+      here = next;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may be on its way into LDS that is given back)
 }
 
 template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
@@ -297,7 +422,9 @@ hipError_t launch_tile(const MxGemmArgs& g, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int64_t tiles_q = g.offsets ? mx_most_tiles(g.T, g.experts, Tile::BQ) : (g.T + Tile::BQ - 1) / Tile::BQ;
   const int64_t tiles = (int64_t)((g.N + Tile::BP - 1) / Tile::BP) * tiles_q;
-  return launch_kernel(kern, dim3((unsigned)tiles), dim3(Tile::NT), Tile::LDS, st, g);
+  MxGemmArgs a = g;
+  a.grid = (uint32_t)(Tile::STAYS && tiles > 256 * Tile::RESIDENT ? 256 * Tile::RESIDENT : tiles);
+  return launch_kernel(kern, dim3(a.grid), dim3(Tile::NT), Tile::LDS, st, a);
 }
 
 }  // namespace
