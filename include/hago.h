@@ -432,12 +432,13 @@ typedef enum { HAGO_MX_FP4 = 0, HAGO_MX_FP8 = 1 } hago_mx_format;
  * (as hago_simquant_codes returns both).
  *   hago_mx_quantize: codes of x.
  *   hago_mx_rmsnorm: h = x + residual (NULL: h = x), codes of
- *     y = h * rsqrt(mean(h^2) + eps) * gamma[col] (NULL: 1), the squares' sum
- *     in 32 bits per thread and 64 across them; residual_out, unless NULL, takes h rounded to
- *     x_t (the norm is of h before that rounding).  It may be residual itself,
- *     or x itself where row_stride == cols.
+ *     y = h * rsqrt(mean(h^2) + eps) * gamma[col] (NULL: 1); residual_out,
+ *     unless NULL, takes h rounded to x_t (the norm is of h before that
+ *     rounding).  It may be residual itself, or x itself where
+ *     row_stride == cols.
  *   hago_mx_silu_mul: x[rows, 2 cols]; codes of g / (1 + exp(-g)) * u with g
- *     the first cols columns of a row and u the others.
+ *     the first cols columns of a row and u the others (g / (1 + exp(-g))
+ *     within a few units of the last place, 0 for g below -88.72).
  * Errors: NULL (x, codes or scales), SHAPE (negative or beyond 2^31 - 129
  * columns or 2^62 elements, row_stride below the columns), DTYPE (x_t), PARAM
  * (format; eps negative or not finite; codes, scales misaligned, or a real

@@ -193,7 +193,7 @@ def _native_module():
                 f"{_NATIVE_PATH} is missing: build it with `python -m paper_2103_14949_amd.build` "
                 "(there is no fallback path)")
         from . import _native as m
-        m.bind({name: C.cast(getattr(L, name), C.c_void_p).value for name in m.entries()}, _check)
+        m.bind({name: C.cast(getattr(L, name), C.c_void_p).value for name in m.entries()}, _check, MX)
         _native = m
     return _native
 
@@ -323,55 +323,28 @@ class MX:
                   torch.empty(rows, wide // 32, dtype=torch.uint8, device=device), fmt, cols)
 
 
-def _mx_out(out, fmt, cols):
-    if out is None:
-        return None, None
-    assert out.fmt == fmt and out.cols == cols
-    return out.codes, out.scales
-
-
-def _mx_result(r, prepare, fmt, cols):
-    """The library's (codes, scales, ...) as (MX, ...), or the MX alone."""
-    t = r.out if prepare else r
-    mx = MX(t[0], t[1], fmt, cols)
-    t = mx if len(t) == 2 else (mx, *t[2:])
-    if not prepare:
-        return t
-    r.out = t   # what its calls return
-    return r
-
-
 def mx_quantize(x, fmt, values=False, out=None, prepare=False):
     """hago_mx_quantize over x[rows, cols] (float32, bfloat16 or float16; rows at any distance): an MX.
 
     values=True, or a tensor like x to take them: (MX, the values that the codes stand for)."""
-    codes, scales = _mx_out(out, fmt, x.shape[-1])
-    r = (_native or _native_module()).mx_quantize(x, fmt, values, codes, scales, prepare)
-    return _mx_result(r, prepare, fmt, x.shape[-1])
+    return (_native or _native_module()).mx_quantize(x, fmt, values, out, prepare)
 
 
 def mx_rmsnorm(x, gamma=None, residual=None, eps=1e-5, fmt=MX_FP8, values=False, out=None, out_residual=None, prepare=False):
     """hago_mx_rmsnorm over x[rows, cols]: an MX of the norm of x, or with a residual (MX, x + residual).
 
     out_residual: the tensor to take the sum, which may be `residual` itself; values as in mx_quantize, returned last."""
-    codes, scales = _mx_out(out, fmt, x.shape[-1])
-    keep = out_residual if out_residual is not None else residual is not None
-    r = (_native or _native_module()).mx_rmsnorm(x, gamma, residual, eps, fmt, values, codes, scales, keep, prepare)
-    return _mx_result(r, prepare, fmt, x.shape[-1])
+    return (_native or _native_module()).mx_rmsnorm(x, gamma, residual, eps, fmt, values, out, out_residual, prepare)
 
 
 def mx_silu_mul(x, fmt, values=False, out=None, prepare=False):
     """hago_mx_silu_mul over x[rows, 2 cols], gate and up side by side: an MX of silu(gate) * up; values as in mx_quantize."""
-    cols = x.shape[-1] // 2
-    codes, scales = _mx_out(out, fmt, cols)
-    r = (_native or _native_module()).mx_silu_mul(x, fmt, values, codes, scales, prepare)
-    return _mx_result(r, prepare, fmt, cols)
+    return (_native or _native_module()).mx_silu_mul(x, fmt, values, out, prepare)
 
 
 def mx_dense(a: MX, w: MX, bias=None, out_dtype=BF16, out=None, prepare=False):
     """hago_mx_dense: a [M,K] (either format), w [N,K] (MX_FP4), bias [N] float32 -> [M,N] of out_dtype (BF16, F16, F32)."""
-    assert w.fmt == MX_FP4 and a.cols == w.cols
-    return (_native or _native_module()).mx_dense(a.codes, a.scales, a.fmt, w.codes, w.scales, a.cols, bias, out_dtype, out, prepare)
+    return (_native or _native_module()).mx_dense(a, w, bias, out_dtype, out, prepare)
 
 
 def mx_dense_grouped(a: MX, w: MX, offsets, rows=None, bias=None, out_dtype=BF16, out=None, prepare=False):
@@ -379,6 +352,4 @@ def mx_dense_grouped(a: MX, w: MX, offsets, rows=None, bias=None, out_dtype=BF16
 
     Result row t belongs to the group e with offsets[e] <= t < offsets[e + 1] and is made of a's row rows[t] (int32
     device tensor; None: row t); bias [E,N] float32.  Returns [T,N]; rows in no group are not written."""
-    assert w.fmt == MX_FP4 and a.cols == w.cols
-    return (_native or _native_module()).mx_dense_grouped(a.codes, a.scales, a.fmt, w.codes, w.scales, a.cols, offsets, rows, bias, out_dtype, out,
-                                                          prepare)
+    return (_native or _native_module()).mx_dense_grouped(a, w, offsets, rows, bias, out_dtype, out, prepare)

@@ -26,8 +26,6 @@ struct MxOut {
   }
 };
 
-// Blocks of 256 threads with 16 elements each.
-constexpr int64_t mx_quantize_blocks(int64_t rows, int64_t cols) { return (rows * (mx_padded(cols) / 8) + 511) / 512; }
 hipError_t launch_mx_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t stride, int format, const MxOut& out, hipStream_t st);
 hipError_t launch_mx_silu_mul(const void* x, int type, int64_t rows, int64_t cols, int64_t stride, int format, const MxOut& out, hipStream_t st);
 hipError_t launch_mx_rmsnorm(const void* x, const void* residual, const void* gamma, int type, int64_t rows, int64_t cols, int64_t stride,

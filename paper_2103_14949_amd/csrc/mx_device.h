@@ -46,6 +46,8 @@ __device__ __forceinline__ void mx_load8(const typename MxElement<TYPE>::type* p
   }
 }
 
+// With the nontemporal hint: values and residuals are read much later than the codes beside them, if at all (norm of 8192 x 4096 bf16
+// with values 54 us without it, 49 so; codes alone of that size in 4 bits, with values, 33 and 23).
 template <int TYPE>
 __device__ __forceinline__ void mx_store8(typename MxElement<TYPE>::type* p, int n, const float (&v)[8]) {
   using T = typename MxElement<TYPE>::type;
@@ -58,7 +60,7 @@ __device__ __forceinline__ void mx_store8(typename MxElement<TYPE>::type* p, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) b.t[i] = (T)v[i];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) reinterpret_cast<mx_u4_any*>(p)[i] = b.u[i];
+    for (int i = 0; i < kVecs; ++i) __builtin_nontemporal_store(b.u[i], reinterpret_cast<mx_u4_any*>(p) + i);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)

@@ -2,7 +2,8 @@
 // addition), and behind a gated activation.
 //
 // A lane takes eight consecutive columns, a quad of lanes a block of 32: the block's largest magnitude takes two lane exchanges, and
-// the codes leave as 4 or 8 consecutive bytes per lane.  All three move bytes and little else.
+// the codes leave as 4 or 8 consecutive bytes per lane.  All three move bytes and little else: 8192 x 8192 fp32 to 4 bits with values in 100 us, norm
+// of 8192 x 4096 bf16 with residual and values in 50, activation of 16384 x 4096 bf16 with values in 84 (5.7, 6.1 and 5.6 TB/s; a copy of 1 GiB 5.0).
 #include "mx_device.h"
 
 namespace hago {
@@ -11,43 +12,47 @@ namespace {
 
 // ---- elementwise: codes of x, or of silu(x[:, :cols]) * x[:, cols:2 cols]
 
-constexpr int kThreads = 256, kPerThread = 2;
+constexpr int kThreads = 256;
 
-// g / (1 + e^-g) * u with the exponential and the division rounded as the host's are (the operator waits for memory
-// all the same).
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+// g / (1 + e^-g) * u within a few units of the last place.  e^-g is 2^t with t = -g log2 e in two parts, the quotient takes one correction; both are
+// scaled by 2^-24, so that the reciprocal of what e^88 leaves is no subnormal number.  Below -88.72, where e^-g is beyond binary32, the result is 0.
+// (16384 x 4096 bf16 with values: 105 us with expf and the division, rounded once each, 100 so, 84 with one place per thread and hinted stores.)
+__device__ __forceinline__ float silu_mul(float g, float u) {
+  constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147182f, kLeast = -88.72f, kDown = 0x1p-24f;
+  const float c = fmaxf(g, kLeast);
+  const float t = c * -kLog2e;
+  const float rest = __builtin_fmaf(c, -kLog2e, -t) - c * kLog2eRest;
+  const float e = __builtin_amdgcn_exp2f(t);
+  const float d = 1.0f + __builtin_fmaf(e, rest * kLn2, e);
+  const float r = __builtin_amdgcn_rcpf(d * kDown);
+  const float q = (c * kDown) * r;
+  const float s = __builtin_fmaf(__builtin_fmaf(-q, d, c) * kDown, r, q);
+  return (g < kLeast ? 0.0f : g > 1e30f ? g : s) * u;
+}
 
+// (One place per thread: two took 0 to 20 % longer, four 10 to 60 % on small tensors.)
 template <int TYPE, int FORMAT, bool GATED>
 __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const void* x, int64_t stride, int64_t rows, int cols, MxOut out) {
   using T = typename MxElement<TYPE>::type;
   const int padded = (cols + 127) & ~127;
   const uint32_t per_row = (uint32_t)padded / 8;
   // the workgroup's first place, in 64 bits; its threads' from there, in 32
-  const uint64_t first = (uint64_t)blockIdx.x * (kThreads * kPerThread);
+  const uint64_t first = (uint64_t)blockIdx.x * kThreads;
   const uint64_t row0 = first >> 32 ? first / per_row : (uint32_t)first / per_row;
-  const uint32_t rest = (uint32_t)(first - row0 * per_row) + threadIdx.x;
-  float v[kPerThread][8], u[kPerThread][8];
-  int64_t row[kPerThread];
-  int col[kPerThread];
+  const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, r = at / per_row;
+  const int64_t row = (int64_t)row0 + r;
+  const int col = (int)(at - r * per_row) * 8;
+  if (row >= rows) return;  // (whole quads: a row's places are a multiple of 16)
+  const T* p = static_cast<const T*>(x) + row * stride + col;
+  float v[8];
+  mx_load8<TYPE>(p, cols - col, v);
+  if constexpr (GATED) {
+    float u[8];
+    mx_load8<TYPE>(p + cols, cols - col, u);
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    const uint32_t at = rest + i * kThreads, r = at / per_row;
-    row[i] = (int64_t)row0 + r;
-    col[i] = (int)(at - r * per_row) * 8;
-    if (row[i] >= rows) continue;
-    const T* p = static_cast<const T*>(x) + row[i] * stride + col[i];
-    mx_load8<TYPE>(p, cols - col[i], v[i]);
-    if constexpr (GATED) mx_load8<TYPE>(p + cols, cols - col[i], u[i]);
+    for (int k = 0; k < 8; ++k) v[k] = silu_mul(v[k], u[k]);
   }
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    if (row[i] >= rows) continue;  // (whole quads: a row's places are a multiple of 16)
-    if constexpr (GATED) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = silu_mul(v[i][k], u[i][k]);
-    }
-    mx_put8<TYPE, FORMAT>(out, row[i], cols, padded, col[i], v[i]);
-  }
+  mx_put8<TYPE, FORMAT>(out, row, cols, padded, col, v);
 }
 
 // ---- norm: h = x + residual, y = h * rsqrt(mean(h^2) + eps) * gamma
@@ -56,34 +61,41 @@ struct NormArgs {
   const void *x, *residual, *gamma;
   void* residual_out;
   MxOut out;
-  int64_t stride;
+  int64_t stride, rows;
   int32_t cols;
   float eps;
 };
 
-// The squares' sum over the workgroup's threads, in 64 bits.
-__device__ __forceinline__ double block_sum(float mine) {
-  __shared__ double parts[16];
-  double s = mine;
-#pragma unroll
-  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-  const int waves = blockDim.x >> 6;
-  if (waves == 1) return s;
-  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = s;
-  __syncthreads();
-  s = 0;
-  for (int w = 0; w < waves; ++w) s += parts[w];
-  return s;
+// Sum over LANES consecutive lanes (16, 32 or 64), in all of them.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  auto add = [&]<int CTRL>() { v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)); };
+  add.template operator()<0xB1>();   // quad_perm 1,0,3,2
+  add.template operator()<0x4E>();   // quad_perm 2,3,0,1
+  add.template operator()<0x141>();  // mirrored within eight lanes
+  add.template operator()<0x140>();  // mirrored within sixteen
+  // (a bit cast of a vector's element takes the first one, whichever is named: the elements are copied out)
+  const auto with = [&](const auto& swap) {
+    const auto s = swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v));
+    const uint32_t a = s[0], b = s[1];
+    v = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+  };
+  if constexpr (LANES >= 32) with([](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane16_swap(a, b, false, false); });
+  if constexpr (LANES >= 64) with([](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane32_swap(a, b, false, false); });
+  return v;
 }
 
-// One workgroup per row, which stays in registers: VECS places of eight columns per thread.  VECS == 0: rows beyond the registers of a
+// LANES lanes per row, 16 to 64 (rows of up to 512 columns, 256 / LANES rows per workgroup), or 0: one workgroup per row.  The row stays in registers,
+// VECS places of eight columns per thread.  VECS == 0: rows beyond the registers of a
 // workgroup are read twice (the second time mostly from the L2).  A place is read, and its residual written, by one thread, so
-// the new residual may lie where the old one, or x, was.
-template <int TYPE, int FORMAT, int VECS>
+// the new residual may lie where the old one, or x, was.  gamma is under way while the squares are added up.
+template <int TYPE, int FORMAT, int VECS, int LANES>
 __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(NormArgs a) {
   using T = typename MxElement<TYPE>::type;
-  const int64_t row = blockIdx.x;
-  const int cols = a.cols, padded = (cols + 127) & ~127, threads = blockDim.x;
+  const int64_t row = LANES ? (int64_t)blockIdx.x * (256 / (LANES ? LANES : 1)) + threadIdx.x / (LANES ? LANES : 1) : blockIdx.x;
+  if (LANES && row >= a.rows) return;  // (all lanes of a row)
+  const int place = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, threads = LANES ? LANES : blockDim.x;
+  const int cols = a.cols, padded = (cols + 127) & ~127;
   const T* x = static_cast<const T*>(a.x) + row * a.stride;
   const T* res = a.residual ? static_cast<const T*>(a.residual) + row * cols : nullptr;
   const T* gamma = static_cast<const T*>(a.gamma);
@@ -101,42 +113,63 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(NormArgs a) {
     for (int k = 0; k < 8; ++k) s = __builtin_fmaf(h[k], h[k], s);
     return s;
   };
-  auto finish = [&](int col, float (&h)[8], float factor) {
+  auto finish = [&](int col, float (&h)[8], float factor, const float (&g)[8]) {
     if (a.residual_out && col < cols) mx_store8<TYPE>(static_cast<T*>(a.residual_out) + row * cols + col, cols - col, h);
-    float g[8];
-    if (gamma) mx_load8<TYPE>(gamma + col, cols - col, g);
 #pragma unroll
     for (int k = 0; k < 8; ++k) h[k] = gamma ? h[k] * factor * g[k] : h[k] * factor;
     mx_put8<TYPE, FORMAT>(a.out, row, cols, padded, col, h);
   };
-  auto factor_of = [&](double sum) { return 1.0f / sqrtf((float)(sum / cols) + a.eps); };
+  auto factor_of = [&](float mine) {
+    float sum;
+    if constexpr (LANES != 0) {
+      sum = lanes_sum<LANES>(mine);
+    } else {
+      __shared__ float parts[16];
+      const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+      sum = lanes_sum<64>(mine);
+      if (waves > 1) {
+        if (lane == 0) parts[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        sum = lanes_sum<16>((lane & 15) < waves ? parts[lane & 15] : 0.0f);
+      }
+    }
+    return 1.0f / sqrtf(sum / (float)cols + a.eps);
+  };
   if constexpr (VECS > 0) {
-    float h[VECS][8];
+    float h[VECS][8], g[VECS][8];
     float sum = 0;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
-      const int col = ((int)threadIdx.x + i * threads) * 8;
-      if (col < padded) {
-        load(col, h[i]);
-        sum = square(h[i], sum);
+      const int col = (place + i * threads) * 8;
+      if (col < padded) load(col, h[i]);
+    }
+    if (gamma) {
+#pragma unroll
+      for (int i = 0; i < VECS; ++i) {
+        const int col = (place + i * threads) * 8;
+        if (col < padded) mx_load8<TYPE>(gamma + col, cols - col, g[i]);
       }
     }
-    const float factor = factor_of(block_sum(sum));
+#pragma unroll
+    for (int i = 0; i < VECS; ++i)
+      if ((place + i * threads) * 8 < padded) sum = square(h[i], sum);
+    const float factor = factor_of(sum);
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
-      const int col = ((int)threadIdx.x + i * threads) * 8;
-      if (col < padded) finish(col, h[i], factor);
+      const int col = (place + i * threads) * 8;
+      if (col < padded) finish(col, h[i], factor, g[i]);
     }
   } else {
-    float h[8], sum = 0;
-    for (int col = (int)threadIdx.x * 8; col < padded; col += threads * 8) {
+    float h[8], g[8], sum = 0;
+    for (int col = place * 8; col < padded; col += threads * 8) {
       load(col, h);
       sum = square(h, sum);
     }
-    const float factor = factor_of(block_sum(sum));
-    for (int col = (int)threadIdx.x * 8; col < padded; col += threads * 8) {
+    const float factor = factor_of(sum);
+    for (int col = place * 8; col < padded; col += threads * 8) {
       load(col, h);
-      finish(col, h, factor);
+      if (gamma) mx_load8<TYPE>(gamma + col, cols - col, g);
+      finish(col, h, factor, g);
     }
   }
 }
@@ -157,12 +190,13 @@ hipError_t by_type(int type, int format, const F& f) {
 template <bool GATED>
 hipError_t quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t stride, int format, const MxOut& out, hipStream_t st) {
   // (a launch holds fewer than 2^32 threads)
-  const int64_t most = max_blocks(kThreads) * (kThreads * kPerThread) / (mx_padded(cols) / 8);
+  const int64_t most = max_blocks(kThreads) * kThreads / (mx_padded(cols) / 8);
   for (int64_t row = 0; row < rows; row += most) {
     const int64_t n = rows - row < most ? rows - row : most;
     const hipError_t e = by_type(type, format, [&]<int TYPE, int FORMAT>() {
       using T = typename MxElement<TYPE>::type;
-      return launch_kernel(mx_quantize_kernel<TYPE, FORMAT, GATED>, dim3((unsigned)mx_quantize_blocks(n, cols)), dim3(kThreads), 0, st,
+      const int64_t blocks = (n * (mx_padded(cols) / 8) + kThreads - 1) / kThreads;
+      return launch_kernel(mx_quantize_kernel<TYPE, FORMAT, GATED>, dim3((unsigned)blocks), dim3(kThreads), 0, st,
                            static_cast<const T*>(x) + row * stride, stride, n, (int)cols, out.from<T>(row, cols, format));
     });
     if (e != hipSuccess) return e;
@@ -183,22 +217,26 @@ hipError_t launch_mx_silu_mul(const void* x, int type, int64_t rows, int64_t col
 hipError_t launch_mx_rmsnorm(const void* x, const void* residual, const void* gamma, int type, int64_t rows, int64_t cols, int64_t stride,
                              float eps, int format, void* residual_out, const MxOut& out, hipStream_t st) {
   const int64_t places = mx_padded(cols) / 8;
+  const int lanes = places <= 16 ? 16 : places <= 32 ? 32 : places <= 64 ? 64 : 0;
   const int vecs = places <= 1024 ? 1 : places <= 2048 ? 2 : places <= 4096 ? 4 : 0;
   const int64_t each = vecs ? (places + vecs - 1) / vecs : 1024;
-  const unsigned threads = (unsigned)((each + 63) / 64 * 64);
-  const int64_t most = max_blocks((int)threads);
+  const unsigned threads = lanes ? 256 : (unsigned)((each + 63) / 64 * 64), per_block = lanes ? 256 / lanes : 1;
+  const int64_t most = max_blocks((int)threads) * per_block;
   for (int64_t row = 0; row < rows; row += most) {
     const int64_t n = rows - row < most ? rows - row : most;
     const hipError_t e = by_type(type, format, [&]<int TYPE, int FORMAT>() {
       using T = typename MxElement<TYPE>::type;
       const T* res = residual ? static_cast<const T*>(residual) + row * cols : nullptr;
       T* res_out = residual_out ? static_cast<T*>(residual_out) + row * cols : nullptr;
-      const NormArgs a{static_cast<const T*>(x) + row * stride, res, gamma, res_out, out.from<T>(row, cols, format), stride, (int32_t)cols, eps};
-      const auto kern = vecs == 1   ? mx_rmsnorm_kernel<TYPE, FORMAT, 1>
-                        : vecs == 2 ? mx_rmsnorm_kernel<TYPE, FORMAT, 2>
-                        : vecs == 4 ? mx_rmsnorm_kernel<TYPE, FORMAT, 4>
-                                    : mx_rmsnorm_kernel<TYPE, FORMAT, 0>;
-      return launch_kernel(kern, dim3((unsigned)n), dim3(threads), 0, st, a);
+      const NormArgs a{static_cast<const T*>(x) + row * stride, res, gamma, res_out, out.from<T>(row, cols, format), stride, n, (int32_t)cols, eps};
+      const auto kern = lanes == 16   ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 16>
+                        : lanes == 32 ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 32>
+                        : lanes == 64 ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 64>
+                        : vecs == 1   ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 0>
+                        : vecs == 2   ? mx_rmsnorm_kernel<TYPE, FORMAT, 2, 0>
+                        : vecs == 4   ? mx_rmsnorm_kernel<TYPE, FORMAT, 4, 0>
+                                      : mx_rmsnorm_kernel<TYPE, FORMAT, 0, 0>;
+      return launch_kernel(kern, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(threads), 0, st, a);
     });
     if (e != hipSuccess) return e;
   }

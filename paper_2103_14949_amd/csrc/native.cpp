@@ -612,60 +612,88 @@ MxRows mx_rows(PyObject* o) {
   return {real_type(t), t.scalar_type(), rows, columns, rows > 1 && columns ? t.stride(0) : columns, t.data_ptr()};
 }
 
-// What such an operator returns, as a tuple: codes, scales, then the residual and the values where they are asked for.
-// `values` is None, True or the tensor to take them.
+PyObject* g_mx = nullptr;  // the binding's class MX(codes, scales, fmt, cols)
+
+// What such an operator returns: an MX, and behind it the residual and the values where they are asked for (a tuple then).
+// `out` is None or an MX whose tensors are taken; residual and values are True, a tensor, or False (values: or None).
 struct MxResults {
   PyObject* all;
   void *codes, *scales, *residual = nullptr, *values = nullptr;
 };
-MxResults mx_results(const at::Tensor& like, const MxRows& x, int64_t cols, int64_t format, PyObject* codes, PyObject* scales, PyObject* residual, PyObject* values) {
-  require_format(format);
-  const int64_t code_shape[2] = {x.rows, mx_code_bytes(cols, format)}, scale_shape[2] = {x.rows, mx_padded(cols) / 32}, shape[2] = {x.rows, cols};
-  given(codes, at::IntArrayRef(code_shape, 2), at::kByte);
-  given(scales, at::IntArrayRef(scale_shape, 2), at::kByte);
+MxResults mx_results(const at::Tensor& like, const MxRows& x, int64_t cols, PyObject* format, PyObject* out, PyObject* residual, PyObject* values) {
+  static PyObject *n_codes = intern("codes"), *n_scales = intern("scales"), *n_fmt = intern("fmt"), *n_cols = intern("cols");
+  const int64_t f = as_int(format);
+  require_format(f);
+  const int64_t code_shape[2] = {x.rows, mx_code_bytes(cols, f)}, scale_shape[2] = {x.rows, mx_padded(cols) / 32}, shape[2] = {x.rows, cols};
   const bool has_residual = residual != Py_False, has_values = values != Py_None && values != Py_False;
-  if (residual != Py_True && has_residual) given(residual, at::IntArrayRef(shape, 2), x.scalar);
-  if (values != Py_True && has_values) given(values, at::IntArrayRef(shape, 2), x.scalar);
-  PyObject* all = PyTuple_New(2 + has_residual + has_values);
-  if (!all) throw Raised{};
-  try {
-    Py_ssize_t i = 0;
-    auto add = [&](PyObject* o, const int64_t* s, at::ScalarType type) {
-      PyObject* t = output(o == Py_True ? Py_None : o, at::IntArrayRef(s, 2), type, like);
-      PyTuple_SET_ITEM(all, i++, t);
-      return tensor(t).data_ptr();
-    };
-    MxResults r{all, add(codes, code_shape, at::kByte), nullptr};
-    r.scales = add(scales, scale_shape, at::kByte);
-    if (has_residual) r.residual = add(residual, shape, x.scalar);
-    if (has_values) r.values = add(values, shape, x.scalar);
-    return r;
-  } catch (...) {
-    Py_DECREF(all);
-    throw;
+  Ref mx, codes, scales, res, val;
+  if (out != Py_None) {
+    require(attr_int(out, n_fmt) == f && attr_int(out, n_cols) == cols);
+    codes.o = PyObject_GetAttr(out, n_codes);
+    scales.o = codes.o ? PyObject_GetAttr(out, n_scales) : nullptr;
+    if (!scales.o) throw Raised{};
+    tensor(codes.o), tensor(scales.o);
+    given(codes.o, at::IntArrayRef(code_shape, 2), at::kByte);
+    given(scales.o, at::IntArrayRef(scale_shape, 2), at::kByte);
+    on_current_device({codes.o, scales.o});
+    Py_INCREF(out);
+    mx.o = out;
   }
+  auto optional = [&](PyObject* o, bool has, Ref& r) {
+    if (!has) return;
+    if (o != Py_True) given(o, at::IntArrayRef(shape, 2), x.scalar), on_current_device({o});
+    r.o = output(o == Py_True ? Py_None : o, at::IntArrayRef(shape, 2), x.scalar, like);
+  };
+  optional(residual, has_residual, res);
+  optional(values, has_values, val);
+  if (!mx.o) {
+    codes.o = output(Py_None, at::IntArrayRef(code_shape, 2), at::kByte, like);
+    scales.o = output(Py_None, at::IntArrayRef(scale_shape, 2), at::kByte, like);
+    Ref c;
+    c.o = PyLong_FromLongLong(cols);
+    PyObject* args[4] = {codes.o, scales.o, format, c.o};
+    mx.o = c.o ? PyObject_Vectorcall(g_mx, args, 4, nullptr) : nullptr;
+    if (!mx.o) throw Raised{};
+  }
+  MxResults r{nullptr, tensor(codes.o).data_ptr(), tensor(scales.o).data_ptr(), has_residual ? tensor(res.o).data_ptr() : nullptr,
+              has_values ? tensor(val.o).data_ptr() : nullptr};
+  auto take = [](Ref& v) {
+    PyObject* o = v.o;
+    v.o = nullptr;
+    return o;
+  };
+  if (!has_residual && !has_values) {
+    r.all = take(mx);
+    return r;
+  }
+  r.all = PyTuple_New(1 + has_residual + has_values);
+  if (!r.all) throw Raised{};
+  Py_ssize_t i = 0;
+  PyTuple_SET_ITEM(r.all, i++, take(mx));
+  if (has_residual) PyTuple_SET_ITEM(r.all, i++, take(res));
+  if (has_values) PyTuple_SET_ITEM(r.all, i++, take(val));
+  return r;
 }
 
-// mx_quantize, mx_silu_mul: (x, format, values, codes, scales, prepare)
+// mx_quantize, mx_silu_mul: (x, format, values, out, prepare)
 template <class Fn>
 PyObject* mx_quantize_with(Fn fn, bool gated, PyObject* const* a, Py_ssize_t n) {
-  need_args(n, 6);
+  need_args(n, 5);
   const MxRows x = mx_rows(a[0]);
-  const int64_t format = as_int(a[1]);
   require(!gated || x.columns % 2 == 0);
-  const int64_t cols = gated ? x.columns / 2 : x.columns;
-  on_current_device({a[0], a[2] == Py_True || a[2] == Py_False ? nullptr : a[2], a[3], a[4]});
-  const bool prepare = as_bool(a[5]);
+  const int64_t cols = gated ? x.columns / 2 : x.columns, format = as_int(a[1]);
+  on_current_device({a[0]});
+  const bool prepare = as_bool(a[4]);
   void* st = stream();
-  const MxResults r = mx_results(tensor(a[0]), x, cols, format, a[3], a[4], Py_False, a[2]);
+  const MxResults r = mx_results(tensor(a[0]), x, cols, a[1], a[3], Py_False, a[2]);
   return issue([=] { return fn(x.src, x.type, x.rows, cols, x.stride, (hago_mx_format)format, r.codes, r.scales, r.values, st); }, r.all, prepare, {a[0]});
 }
 PyObject* f_mx_quantize(PyObject* const* a, Py_ssize_t n) { return mx_quantize_with(L.hago_mx_quantize, false, a, n); }
 PyObject* f_mx_silu_mul(PyObject* const* a, Py_ssize_t n) { return mx_quantize_with(L.hago_mx_silu_mul, true, a, n); }
 
-// (x, gamma, residual, eps, format, values, codes, scales, out_residual, prepare); out_residual: False where none is wanted
+// (x, gamma, residual, eps, format, values, out, out_residual, prepare); out_residual None: a new tensor where there is a residual
 PyObject* f_mx_rmsnorm(PyObject* const* a, Py_ssize_t n) {
-  need_args(n, 10);
+  need_args(n, 9);
   const MxRows x = mx_rows(a[0]);
   const int64_t shape[2] = {x.rows, x.columns};
   given(a[1], at::IntArrayRef(&x.columns, 1), x.scalar);
@@ -673,78 +701,87 @@ PyObject* f_mx_rmsnorm(PyObject* const* a, Py_ssize_t n) {
   const double eps = PyFloat_AsDouble(a[3]);
   if (eps == -1.0 && PyErr_Occurred()) throw Raised{};
   const int64_t format = as_int(a[4]);
-  auto maybe = [](PyObject* o) { return o == Py_True || o == Py_False ? nullptr : o; };
-  on_current_device({a[0], a[1], a[2], maybe(a[5]), a[6], a[7], maybe(a[8])});
+  on_current_device({a[0], a[1], a[2]});
   const void *gamma = pointer(a[1]), *res = pointer(a[2]);
-  const bool prepare = as_bool(a[9]);
+  const bool prepare = as_bool(a[8]);
+  PyObject* keep = a[7] != Py_None ? a[7] : a[2] != Py_None ? Py_True : Py_False;
   void* st = stream();
-  const MxResults r = mx_results(tensor(a[0]), x, x.columns, format, a[6], a[7], a[8], a[5]);
+  const MxResults r = mx_results(tensor(a[0]), x, x.columns, a[4], a[6], keep, a[5]);
   return issue([=] { return L.hago_mx_rmsnorm(x.src, res, gamma, x.type, x.rows, x.columns, x.stride, (float)eps, (hago_mx_format)format, r.residual, r.codes,
                                               r.scales, r.values, st); },
                r.all, prepare, {a[0], a[1], a[2]});
 }
 
+// An MX: its tensors (references of its own) and what they say.
 struct MxOperand {
-  const void *codes, *scales;
-  int64_t rows;
+  Ref codes, scales;
+  int64_t format, cols, rows, groups;
+  const void* code_ptr() const { return tensor(codes.o).data_ptr(); }
+  const void* scale_ptr() const { return tensor(scales.o).data_ptr(); }
+  // [rows, cols], or with dims == 3 [groups, rows, cols]
+  MxOperand(PyObject* mx, int64_t dims) {
+    static PyObject *n_codes = intern("codes"), *n_scales = intern("scales"), *n_fmt = intern("fmt"), *n_cols = intern("cols");
+    format = attr_int(mx, n_fmt), cols = attr_int(mx, n_cols);
+    codes.o = PyObject_GetAttr(mx, n_codes);
+    scales.o = codes.o ? PyObject_GetAttr(mx, n_scales) : nullptr;
+    if (!scales.o) throw Raised{};
+    require_format(format);
+    require(cols >= 0);
+    const at::Tensor &c = tensor(codes.o), &s = tensor(scales.o);
+    require(c.dim() == dims && s.dim() == dims && c.scalar_type() == at::kByte && s.scalar_type() == at::kByte && c.is_contiguous() && s.is_contiguous());
+    require(c.size(dims - 1) == mx_code_bytes(cols, format) && s.size(dims - 1) == mx_padded(cols) / 32 && c.size(dims - 2) == s.size(dims - 2));
+    require(dims == 2 || c.size(0) == s.size(0));
+    rows = c.size(dims - 2), groups = dims == 3 ? c.size(0) : 1;
+  }
 };
-// codes and scales of [.., rows, cols] in a format
-MxOperand mx_operand(PyObject* codes, PyObject* scales, int64_t dims, int64_t cols, int64_t format) {
-  require_format(format);
-  require(cols >= 0);
-  const at::Tensor &c = tensor(codes), &s = tensor(scales);
-  require(c.dim() == dims && s.dim() == dims && c.scalar_type() == at::kByte && s.scalar_type() == at::kByte && c.is_contiguous() && s.is_contiguous());
-  require(c.size(dims - 1) == mx_code_bytes(cols, format) && s.size(dims - 1) == mx_padded(cols) / 32 && c.size(dims - 2) == s.size(dims - 2));
-  require(dims == 2 || c.size(0) == s.size(0));
-  return {c.data_ptr(), s.data_ptr(), c.size(dims - 2)};
-}
 
-// (a_codes, a_scales, a_format, w_codes, w_scales, cols, bias, out_dtype, out, prepare)
+// (a, w, bias, out_dtype, out, prepare)
 PyObject* f_mx_dense(PyObject* const* a, Py_ssize_t n) {
-  need_args(n, 10);
-  const int64_t format = as_int(a[2]), K = as_int(a[5]), type = as_int(a[7]);
-  const MxOperand act = mx_operand(a[0], a[1], 2, K, format), w = mx_operand(a[3], a[4], 2, K, HAGO_MX_FP4);
-  const int64_t M = act.rows, N = w.rows, shape[2] = {M, N};
-  given(a[6], at::IntArrayRef(&N, 1), at::kFloat);
-  given(a[8], at::IntArrayRef(shape, 2), scalar_type(type));
-  on_current_device({a[0], a[1], a[3], a[4], a[6], a[8]});
-  const float* bias = static_cast<const float*>(pointer(a[6]));
-  const bool prepare = as_bool(a[9]);
+  need_args(n, 6);
+  const MxOperand act(a[0], 2), w(a[1], 2);
+  require(w.format == HAGO_MX_FP4 && w.cols == act.cols);
+  const int64_t M = act.rows, N = w.rows, K = act.cols, shape[2] = {M, N}, format = act.format, type = as_int(a[3]);
+  given(a[2], at::IntArrayRef(&N, 1), at::kFloat);
+  given(a[4], at::IntArrayRef(shape, 2), scalar_type(type));
+  on_current_device({act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[4]});
+  const float* bias = static_cast<const float*>(pointer(a[2]));
+  const bool prepare = as_bool(a[5]);
+  const void *ac = act.code_ptr(), *as = act.scale_ptr(), *wc = w.code_ptr(), *ws = w.scale_ptr();
   void* st = stream();
-  PyObject* out = output(a[8], at::IntArrayRef(shape, 2), scalar_type(type), tensor(a[0]));
+  PyObject* out = output(a[4], at::IntArrayRef(shape, 2), scalar_type(type), tensor(act.codes.o));
   void* dst = pointer(out);
-  return issue([=] { return L.hago_mx_dense(act.codes, act.scales, (hago_mx_format)format, w.codes, w.scales, bias, M, N, K, (hago_dtype)type, dst, st); }, out,
-               prepare, {a[0], a[1], a[3], a[4], a[6]});
+  return issue([=] { return L.hago_mx_dense(ac, as, (hago_mx_format)format, wc, ws, bias, M, N, K, (hago_dtype)type, dst, st); }, out, prepare,
+               {act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2]});
 }
 
-// (a_codes, a_scales, a_format, w_codes, w_scales, cols, offsets, rows, bias, out_dtype, out, prepare)
+// (a, w, offsets, rows, bias, out_dtype, out, prepare)
 PyObject* f_mx_dense_grouped(PyObject* const* a, Py_ssize_t n) {
-  need_args(n, 12);
-  const int64_t format = as_int(a[2]), K = as_int(a[5]), type = as_int(a[9]);
-  const MxOperand act = mx_operand(a[0], a[1], 2, K, format), w = mx_operand(a[3], a[4], 3, K, HAGO_MX_FP4);
-  const int64_t E = tensor(a[3]).size(0), N = w.rows, entries = E + 1, bias_shape[2] = {E, N};
-  tensor(a[6]);
-  given(a[6], at::IntArrayRef(&entries, 1), at::kInt);
+  need_args(n, 8);
+  const MxOperand act(a[0], 2), w(a[1], 3);
+  require(w.format == HAGO_MX_FP4 && w.cols == act.cols);
+  const int64_t E = w.groups, N = w.rows, K = act.cols, entries = E + 1, bias_shape[2] = {E, N}, format = act.format, type = as_int(a[5]);
+  tensor(a[2]);
+  given(a[2], at::IntArrayRef(&entries, 1), at::kInt);
   int64_t T = act.rows;
-  if (a[7] != Py_None) {
-    require(tensor(a[7]).dim() == 1);
-    T = tensor(a[7]).size(0);
-    given(a[7], at::IntArrayRef(&T, 1), at::kInt);
+  if (a[3] != Py_None) {
+    require(tensor(a[3]).dim() == 1);
+    T = tensor(a[3]).size(0);
+    given(a[3], at::IntArrayRef(&T, 1), at::kInt);
   }
   const int64_t shape[2] = {T, N};
-  given(a[8], at::IntArrayRef(bias_shape, 2), at::kFloat);
-  given(a[10], at::IntArrayRef(shape, 2), scalar_type(type));
-  on_current_device({a[0], a[1], a[3], a[4], a[6], a[7], a[8], a[10]});
-  const int32_t *offsets = static_cast<const int32_t*>(pointer(a[6])), *index = static_cast<const int32_t*>(pointer(a[7]));
-  const float* bias = static_cast<const float*>(pointer(a[8]));
-  const bool prepare = as_bool(a[11]);
+  given(a[4], at::IntArrayRef(bias_shape, 2), at::kFloat);
+  given(a[6], at::IntArrayRef(shape, 2), scalar_type(type));
+  on_current_device({act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[3], a[4], a[6]});
+  const int32_t *offsets = static_cast<const int32_t*>(pointer(a[2])), *index = static_cast<const int32_t*>(pointer(a[3]));
+  const float* bias = static_cast<const float*>(pointer(a[4]));
+  const bool prepare = as_bool(a[7]);
+  const void *ac = act.code_ptr(), *as = act.scale_ptr(), *wc = w.code_ptr(), *ws = w.scale_ptr();
   const int64_t a_rows = act.rows;
   void* st = stream();
-  PyObject* out = output(a[10], at::IntArrayRef(shape, 2), scalar_type(type), tensor(a[0]));
+  PyObject* out = output(a[6], at::IntArrayRef(shape, 2), scalar_type(type), tensor(act.codes.o));
   void* dst = pointer(out);
-  return issue([=] { return L.hago_mx_dense_grouped(act.codes, act.scales, (hago_mx_format)format, a_rows, index, w.codes, w.scales, bias, offsets, T, E, N, K,
-                                                    (hago_dtype)type, dst, st); },
-               out, prepare, {a[0], a[1], a[3], a[4], a[6], a[7], a[8]});
+  return issue([=] { return L.hago_mx_dense_grouped(ac, as, (hago_mx_format)format, a_rows, index, wc, ws, bias, offsets, T, E, N, K, (hago_dtype)type, dst, st); },
+               out, prepare, {act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[3], a[4]});
 }
 
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
@@ -758,9 +795,9 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind({name: address}, check)
+// bind({name: address}, check, MX)
 PyObject* f_bind(PyObject* const* a, Py_ssize_t n) {
-  need_args(n, 2);
+  need_args(n, 3);
   Library lib;
 #define X(name)                                                        \
   {                                                                    \
@@ -776,6 +813,8 @@ PyObject* f_bind(PyObject* const* a, Py_ssize_t n) {
   L = lib;
   Py_INCREF(a[1]);
   Py_XSETREF(g_check, a[1]);
+  Py_INCREF(a[2]);
+  Py_XSETREF(g_mx, a[2]);
   Py_RETURN_NONE;
 }
 
