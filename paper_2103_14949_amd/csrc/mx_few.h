@@ -4,6 +4,11 @@
 // sums meet in LDS and are added in the wavefronts' order.  Operands of v_mfma_scale_f32_16x16x128_f8f6f4, measured: lane l has row l % 16; of 4-bit codes
 // the 16 bytes of k = 32 (l / 16) on, of 8-bit codes the 16 bytes of k = 16 (l / 16) on and of k = 64 + 16 (l / 16) on; its scale is the one of
 // k = 32 (l / 16) on.  The loads of a chunk go out together: four pieces of 64 bytes of a row (two lines), 16 bytes of its scales.
+//
+// What bounds it: the weights' bytes, and how many of them are under way.  Where there is a workgroup for every CU and no more, 16 wavefronts each have 4 or 8 KB of a
+// chunk so; weights not in the last-level cache, us with 8 and with 16: a row through 8192 x 8192 12.3, 11.1 (3.2 TB/s; 8.5 out of the cache), 8 rows through 4096
+// features of 14336 k 12.7, 11.3.  The next chunk's loads behind the ones of this chunk give as much there (11.4, 10.9), and their registers cost more
+// where there are many workgroups (16 rows of 60 experts 31 us, 44 so).  Nontemporal loads of the weights took longer (30, 36).
 #pragma once
 
 #include "mx_gemm.h"

@@ -24,16 +24,18 @@ struct MxShape {
   float fixed, each, alone, step;
   float step_row;  // few rows: more per stage (of 512 k there) for the activations of 16 rows
 };
-constexpr int kShapes = 11;
+constexpr int kShapes = 13;
 constexpr MxShape kMxShapes[2][kShapes] = {
-    {{256, 256, 0, 0.00f, 6.25f, 0.81f, 1.21f, 0}, {128, 128, 0, 3.65f, 1.73f, 0.63f, 0.56f, 0}, {128, 64, 0, 3.66f, 0.94f, 0.53f, 0.42f, 0},
-     {64, 64, 0, 2.72f, 0.56f, 0.33f, 0.28f, 0}, {64, 32, 0, 2.86f, 0.75f, 0.29f, 0.21f, 0},
-     {16, 16, 4, 2.615f, 0.100f, 0.343f, 0.195f, 0.017f}, {16, 16, 8, 2.527f, 0.303f, 0.553f, 0.184f, 0.007f}, {32, 16, 2, 3.148f, 0.000f, 0.295f, 0.366f, 0.029f},
-     {32, 16, 4, 2.807f, 0.195f, 0.271f, 0.294f, 0.049f}, {32, 16, 8, 2.392f, 0.607f, 0.776f, 0.291f, 0.015f}, {32, 32, 16, 1.057f, 3.026f, 2.788f, 0.193f, 0.080f}},
-    {{256, 128, 0, 0.33f, 5.60f, 0.93f, 1.23f, 0}, {128, 128, 0, 1.73f, 3.93f, 0.87f, 0.82f, 0}, {128, 64, 0, 3.58f, 1.19f, 0.69f, 0.51f, 0},
-     {64, 64, 0, 2.65f, 0.75f, 0.47f, 0.34f, 0}, {64, 32, 0, 2.61f, 1.16f, 0.39f, 0.27f, 0},
-     {16, 16, 4, 2.666f, 0.028f, 0.336f, 0.237f, 0.095f}, {16, 16, 8, 2.572f, 0.251f, 0.577f, 0.218f, 0.095f}, {32, 16, 2, 3.063f, 0.000f, 0.300f, 0.390f, 0.104f},
-     {32, 16, 4, 2.891f, 0.136f, 0.478f, 0.338f, 0.112f}, {32, 16, 8, 2.484f, 0.559f, 0.333f, 0.335f, 0.073f}, {32, 32, 16, 0.769f, 3.041f, 3.558f, 0.301f, 0.144f}}};
+    {{256, 256, 0, 0.00f, 6.23f, 0.82f, 1.21f, 0}, {128, 128, 0, 3.62f, 1.74f, 0.48f, 0.56f, 0}, {128, 64, 0, 3.66f, 0.93f, 0.54f, 0.42f, 0},
+     {64, 64, 0, 2.72f, 0.56f, 0.34f, 0.28f, 0}, {64, 32, 0, 2.86f, 0.74f, 0.29f, 0.21f, 0}, {16, 16, 4, 2.602f, 0.101f, 0.313f, 0.197f, 0.015f},
+     {16, 16, 8, 2.509f, 0.302f, 0.494f, 0.183f, 0.009f}, {32, 16, 2, 3.202f, 0.000f, 0.153f, 0.342f, 0.050f}, {32, 16, 4, 2.789f, 0.196f, 0.139f, 0.292f, 0.052f},
+     {32, 16, 8, 2.332f, 0.609f, 0.984f, 0.294f, 0.015f}, {32, 32, 16, 1.024f, 3.031f, 3.269f, 0.192f, 0.081f}, {16, 16, 16, 1.996f, 0.866f, 0.300f, 0.184f, 0.000f},
+     {32, 16, 16, 1.628f, 1.577f, 0.773f, 0.266f, 0.042f}},
+    {{256, 128, 0, 0.29f, 5.61f, 0.46f, 1.23f, 0}, {128, 128, 0, 1.69f, 3.96f, 0.31f, 0.82f, 0}, {128, 64, 0, 3.56f, 1.19f, 0.70f, 0.52f, 0},
+     {64, 64, 0, 2.65f, 0.75f, 0.47f, 0.34f, 0}, {64, 32, 0, 2.60f, 1.16f, 0.39f, 0.27f, 0}, {16, 16, 4, 2.657f, 0.028f, 0.302f, 0.239f, 0.093f},
+     {16, 16, 8, 2.526f, 0.252f, 0.565f, 0.223f, 0.090f}, {32, 16, 2, 3.043f, 0.000f, 0.300f, 0.383f, 0.112f}, {32, 16, 4, 2.858f, 0.136f, 0.462f, 0.345f, 0.108f},
+     {32, 16, 8, 2.458f, 0.559f, 0.910f, 0.337f, 0.073f}, {32, 32, 16, 0.760f, 3.036f, 3.549f, 0.301f, 0.146f}, {16, 16, 16, 2.056f, 0.844f, 0.696f, 0.230f, 0.054f},
+     {32, 16, 16, 1.591f, 1.627f, 1.162f, 0.310f, 0.112f}}};
 
 int pick_shape(const MxGemmArgs& g, int a_format) {
   const double k = (double)mx_padded(g.K);
@@ -66,7 +68,7 @@ hipError_t launch_shape(const MxGemmArgs& g, int shape, hipStream_t st) {
     case 2: return launch_tile<FA, 2, 2, 2, 1, 2>(g, st);
     case 3: return launch_tile<FA, 2, 2, 1, 1, 2>(g, st);
     case 4: return launch_tile<FA, 2, 1, 1, 1, 4>(g, st);
-    case 5: case 6: return launch_few<FA, 1, 1>(g, kMxShapes[FA][shape].waves, st);
+    case 5: case 6: case 11: return launch_few<FA, 1, 1>(g, kMxShapes[FA][shape].waves, st);
     case 10: return launch_few<FA, 2, 2>(g, kMxShapes[FA][shape].waves, st);
     default: return launch_few<FA, 2, 1>(g, kMxShapes[FA][shape].waves, st);
   }

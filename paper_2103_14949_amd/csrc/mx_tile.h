@@ -50,7 +50,6 @@ struct MxTile {
   static constexpr int LDS = !BY_LDS || SLOTS * STAGE > NW * 32 * PITCH ? SLOTS * STAGE : NW * 32 * PITCH;
   // A workgroup goes from tile to tile; the next one's first stages are under way while a tile's results leave.
   static constexpr bool STAYS = !BY_LDS && SLOTS == 2 && TP * TQ < 8;
-  static constexpr bool EARLY = TP * TQ < 8;  // its rows are looked up a tile ahead, where registers allow
   static constexpr int RESIDENT = 160 * 1024 / LDS < 16 / NW ? 160 * 1024 / LDS : 16 / NW;  // workgroups that a CU holds
 };
 
@@ -218,8 +217,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
         const int r = (wave + NW * d) * 8 + lrow;
         voff[d] = r < np ? (uint32_t)r * wbytes + lck : kOob;
       } else {
-        constexpr int kPlane = PLANES == 1 ? 0 : LQ;  // loads of a plane
-        const int e = d - GP / NW, plane = kPlane ? e / kPlane : 0, r = picked.q[kPlane ? e % kPlane : e];
+        constexpr int kPlane = LQ;  // loads of a plane
+        const int e = d - GP / NW, plane = e / kPlane, r = picked.q[e % kPlane];
         voff[d] = r >= 0 ? (uint32_t)r * abytes + lck + (uint32_t)plane * 128 : kOob;
       }
     }
@@ -251,7 +250,6 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   static_assert(PLANES == 1 || (BQ / 8) % NW == 0, "a load's plane is the same in every wavefront");
   template_int<0> i0;
 
-  mx_v16f acc[TP][TQ];
   // fragment addresses inside a stage
   const int frow = lane & 31;
   auto chunk_at = [&](int c) { return (c ^ swz<128>(frow & 15)) * 16; };
@@ -289,7 +287,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   };
   // Group H of a stage: multiply its set of fragments, behind the instructions go the reads of the next group's set (from `next`) and of
   // the next half's scales in front of it, and in the last group the loads of stage `dma_stage`.
-  auto multiply = [&](auto hconst, auto ring, const uint8_t* next, int dma_stage) {
+  auto multiply = [&](mx_v16f (&acc)[TP][TQ], auto hconst, const uint8_t* next, int dma_stage, auto ring) {
     constexpr int H = decltype(hconst)::value, S = H & 1;
     constexpr int reads = NR + (H % 2 ? TP + TQ : 0), each = (reads + NM - 1) / NM > 2 ? (reads + NM - 1) / NM : 2;
     [&]<int... Mi>(std::integer_sequence<int, Mi...>) {
@@ -317,28 +315,33 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   constexpr int kStores16 = TQ * TP / 2 * 4, kStores32 = 2 * kStores16;
   int stores = 0;  // of the last tile's results, behind the loads of this one's first two stages
   bool first = true, more = false;
-  auto stage_body = [&](int kt, auto ring) {
-    constexpr int R = decltype(ring)::value;
-    const uint8_t* here = smem + R * STAGE;
-    const uint8_t* other = smem + (R + 1) % SLOTS * STAGE;
-    const bool blank = Tile::STAYS && kt >= KT;
-    if (!blank) {
-      multiply(template_int<0>{}, ring, here, 0);
-      multiply(template_int<1>{}, ring, here, 0);
-      multiply(template_int<2>{}, ring, here, 0);
-    }
-    // the next stage has landed; the stores behind it need not have
+  // Before a stage's last group: the next stage has landed (the stores behind it need not have), and every wavefront is done with this one's slot.
+  auto meet = [&](int kt) {
     if (Tile::STAYS && kt == 0 && stores == kStores16) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStores16) : "memory");
     else if (Tile::STAYS && kt == 0 && stores == kStores32) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStores32) : "memory");
     else asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 2) * ISSUES) : "memory");
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    // (stages behind the last one are the next tile's)
-    const int fetch = Tile::STAYS && more && kt + SLOTS >= stages ? kt + SLOTS - stages : kt + SLOTS;
-    if (!blank) multiply(template_int<3>{}, ring, other, fetch);
-    else issue(fetch, ring, i0, template_int<ISSUES>{});
   };
+  // the stage that goes into a stage's slot behind it (stages behind the last one are the next tile's)
+  auto fetched = [&](int kt) { return Tile::STAYS && more && kt + SLOTS >= stages ? kt + SLOTS - stages : kt + SLOTS; };
+  auto stage_body = [&](mx_v16f (&acc)[TP][TQ], int kt, auto ring) {
+    constexpr int R = decltype(ring)::value;
+    const uint8_t* here = smem + R * STAGE;
+    const uint8_t* other = smem + (R + 1) % SLOTS * STAGE;
+    multiply(acc, template_int<0>{}, here, 0, ring);
+    multiply(acc, template_int<1>{}, here, 0, ring);
+    multiply(acc, template_int<2>{}, here, 0, ring);
+    meet(kt);
+    multiply(acc, template_int<3>{}, other, fetched(kt), ring);
+  };
+  // a stage of which nothing is this wavefront's
+  auto idle_stage = [&](int kt, auto ring) {
+    meet(kt);
+    issue(fetched(kt), ring, i0, template_int<ISSUES>{});
+  };
+
   auto by_type = [&](const auto& f) {
     if (g.type == kMxF32) f.template operator()<kMxF32>();
     else if (g.type == kMxBf16) f.template operator()<kMxBf16>();
@@ -348,6 +351,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
   Place here = place_of(id);
   bind(here, pick_rows(here));
   [&]<int... I>(std::integer_sequence<int, I...>) { (issue(I, template_int<I>{}, i0, template_int<ISSUES>{}), ...); }(std::make_integer_sequence<int, SLOTS>{});
+  static_assert(SLOTS * ISSUES <= 63, "loads that can be counted");
   for (;;) {
     // the next tile's rows are looked up now and used when this one's loads have all gone out
     more = Tile::STAYS && id + g.grid < count;
@@ -355,60 +359,82 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) 
     Picked picked;
     if (more) next = place_of(id + g.grid);
     if (more) picked = pick_rows(next);
-
-    if (g.bias) {
-      const float* bias = g.bias + (int64_t)here.rows.expert * g.N;
-#pragma unroll
-      for (int i = 0; i < TP; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float b = bias[min(here.p0 + (wp * TP + i) * 32 + 8 * (r / 4) + 4 * half + r % 4, g.N - 1)];
-#pragma unroll
-          for (int j = 0; j < TQ; ++j) acc[i][j][r] = b;
-        }
-    } else {
-#pragma unroll
-      for (int i = 0; i < TP; ++i)
-#pragma unroll
-        for (int j = 0; j < TQ; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-    }
-
-    if (first) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * ISSUES) : "memory");  // stage 0 (of a later tile: waited for in the last stage)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int r = 0; r < NR; ++r) read(smem, i0, i0, r);
-#pragma unroll
-    for (int r = 0; r < TP + TQ; ++r) read_scale(smem, i0, r);
-    shift_scales(i0);
-    static_assert(SLOTS * ISSUES <= 63, "loads that can be counted");
-    for (int kt = 0; kt < stages; kt += SLOTS) {
-      if (more && kt + SLOTS >= stages) bind(next, Tile::EARLY ? picked : pick_rows(next));
+    auto bind_next = [&](int kt) {
+      if (more && kt + SLOTS >= stages) bind(next, picked);
+    };
+    auto start = [&] {
+      if (first) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * ISSUES) : "memory");  // stage 0 (of a later tile: waited for in the last stage)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    auto drain = [&] {  // (the stages beyond K have to land before the slots are used for something else)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    };
+    auto round = [&](int kt, int end, const auto& body) {  // stages kt .. end - 1, at most one a slot
       [&]<int... I>(std::integer_sequence<int, I...>) {
         ([&] {
-          if (I == 0 || Tile::STAYS || kt + I < stages) stage_body(kt + I, template_int<I>{});
+          if (I == 0 || kt + I < end) body(kt + I, template_int<I>{});
         }(), ...);
       }(std::make_integer_sequence<int, SLOTS>{});
-    }
-    // The next tile's first stages are on their way into LDS, or in it, while the results leave.
+    };
     const int n0 = here.p0 + wp * TP * 32, nq = min(here.rows.end - here.rows.row, BQ);
-    if constexpr (Tile::BY_LDS) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the stages beyond K; before LDS is used for something else)
-      __syncthreads();
-      uint8_t* mine = smem + wave * 32 * Tile::PITCH;
-      by_type([&]<int TYPE>() { leave_by_lds<TYPE, TP, TQ>(g, acc, here.rows.row, wq * TQ * 32, nq, n0, lane, mine); });
-      return;
+    // A wavefront that has none of a ragged tile's rows or features loads and waits with the others, no more.  (Its way and the others' part
+    // before there are sums: where they meet with sums in registers, the compiler keeps two sets of them.)
+    if (wq * TQ * 32 >= nq || n0 >= g.N) {
+      start();
+      for (int kt = 0; kt < stages; kt += SLOTS) {
+        bind_next(kt);
+        round(kt, stages, idle_stage);
+      }
+      if (Tile::BY_LDS) drain();
     } else {
-      by_type([&]<int TYPE>() { leave_by_quads<TYPE, TP, TQ>(g, acc, here.rows.row, wq * TQ * 32, nq, n0, lane); });
-      if (!more) break;
-      // (every lane of a whole tile stores, so that the stores can be counted)
-      stores = nq == BQ && n0 + TP * 32 <= g.N ? (g.type == kMxF32 ? kStores32 : kStores16) : 0;
-      first = false;
-      id += g.grid;
-      here = next;
+      // the sums start from the bias (of features beyond the last one, which nobody stores: the last one's)
+      mx_v16f acc[TP][TQ];
+      if (g.bias) {
+        const float* bias = g.bias + (int64_t)here.rows.expert * g.N;
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float b = bias[min(n0 + i * 32 + 8 * (r / 4) + 4 * half + r % 4, g.N - 1)];
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) acc[i][j][r] = b;
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+#pragma unroll
+          for (int j = 0; j < TQ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+      }
+      start();
+#pragma unroll
+      for (int r = 0; r < NR; ++r) read(smem, i0, i0, r);
+#pragma unroll
+      for (int r = 0; r < TP + TQ; ++r) read_scale(smem, i0, r);
+      shift_scales(i0);
+      auto work = [&](int kt, auto ring) { stage_body(acc, kt, ring); };
+      for (int kt = 0; kt < KT; kt += SLOTS) {
+        bind_next(kt);
+        round(kt, KT, work);
+      }
+      if constexpr (Tile::BY_LDS) {
+        drain();
+        uint8_t* mine = smem + wave * 32 * Tile::PITCH;
+        by_type([&]<int TYPE>() { leave_by_lds<TYPE, TP, TQ>(g, acc, here.rows.row, wq * TQ * 32, nq, n0, lane, mine); });
+      } else {
+        if (KT < stages) idle_stage(KT, template_int<1>{});
+        by_type([&]<int TYPE>() { leave_by_quads<TYPE, TP, TQ>(g, acc, here.rows.row, wq * TQ * 32, nq, n0, lane); });
+      }
     }
+    if (!more) break;
+    // (every lane of a whole tile stores, so that the stores can be counted)
+    stores = nq == BQ && n0 + TP * 32 <= g.N ? (g.type == kMxF32 ? kStores32 : kStores16) : 0;
+    first = false;
+    id += g.grid;
+    here = next;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may be on its way into LDS that is given back)
 }

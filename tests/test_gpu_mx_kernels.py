@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 import paper_2103_14949_amd as hago
 import test_gpu_mx as t
 
-KERNELS = range(11)
+KERNELS = range(13)
 
 
 @pytest.fixture(params=KERNELS)
