@@ -1,4 +1,4 @@
-"""MI355X-native quantized operators of HAGO (arXiv 2103.14949).
+"""MI355X-native quantized operators of HAGO (arXiv 2103.14949), and microscaled operators for transformers.
 
 The package is a thin binding over ``libhago.so`` (hand-written HIP
 kernels behind a C ABI, see ``include/hago.h``).  Every operator runs in those
