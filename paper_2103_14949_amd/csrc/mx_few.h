@@ -20,7 +20,8 @@ namespace {
 constexpr int kMostFewWaves = 16;
 
 template <int FA, int TP, int TQ>
-__global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(MxGemmArgs g) {
+__global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(HAGO_MX_GEMM_PARAMETERS) {
+  const MxGemmArgs g = HAGO_MX_GEMM_STRUCT;
   constexpr int BP = 16 * TP, BQ = 16 * TQ, PLANES = FA == kMxFp8 ? 2 : 1, STEPS = 4;
   extern __shared__ __attribute__((aligned(16))) float sums[];
   const int lane = threadIdx.x & 63, part = lane >> 4;
@@ -34,18 +35,18 @@ __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(MxGemmArgs g
   const int padded = (g.K + 127) & ~127, steps = padded / 128;
   const int wbytes = padded / 2, abytes = FA == kMxFp4 ? wbytes : padded, sbytes = padded / 32;
 
-  const uint8_t *w[TP], *ws[TP], *a[TQ], *as[TQ];
+  const uint8_t *wr[TP], *wsr[TP], *ar[TQ], *asr[TQ];  // the lane's rows
 #pragma unroll
   for (int i = 0; i < TP; ++i) {
     const int64_t r = (int64_t)rows.expert * g.N + min(p0 + 16 * i + (lane & 15), g.N - 1);
-    w[i] = g.w + r * wbytes + part * 16;
-    ws[i] = g.w_scale + r * sbytes;
+    wr[i] = g.w + r * wbytes + part * 16;
+    wsr[i] = g.w_scale + r * sbytes;
   }
 #pragma unroll
   for (int j = 0; j < TQ; ++j) {
     const int64_t r = mx_row_of(g, rows.row + min(16 * j + (lane & 15), nq - 1));
-    a[j] = g.a + r * abytes + part * 16;
-    as[j] = g.a_scale + r * sbytes;
+    ar[j] = g.a + r * abytes + part * 16;
+    asr[j] = g.a_scale + r * sbytes;
   }
   mx_v4f acc[TP][TQ];
 #pragma unroll
@@ -75,19 +76,19 @@ __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(MxGemmArgs g
     for (int u = 0; u < STEPS; ++u) {
       const int at = whole ? step + u : min(step + u, steps - 1);
 #pragma unroll
-      for (int i = 0; i < TP; ++i) wf[u][i] = *reinterpret_cast<const mx_v4i*>(w[i] + at * 64);
+      for (int i = 0; i < TP; ++i) wf[u][i] = *reinterpret_cast<const mx_v4i*>(wr[i] + at * 64);
     }
 #pragma unroll
-    for (int i = 0; i < TP; ++i) wsf[i] = scales(ws[i], step, whole);
+    for (int i = 0; i < TP; ++i) wsf[i] = scales(wsr[i], step, whole);
 #pragma unroll
-    for (int j = 0; j < TQ; ++j) asf[j] = scales(as[j], step, whole);
+    for (int j = 0; j < TQ; ++j) asf[j] = scales(asr[j], step, whole);
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) {
       const int at = whole ? step + u : min(step + u, steps - 1);
 #pragma unroll
       for (int j = 0; j < TQ; ++j)
 #pragma unroll
-        for (int h = 0; h < PLANES; ++h) af[u][j * PLANES + h] = *reinterpret_cast<const mx_v4i*>(a[j] + at * 64 * PLANES + h * 64);
+        for (int h = 0; h < PLANES; ++h) af[u][j * PLANES + h] = *reinterpret_cast<const mx_v4i*>(ar[j] + at * 64 * PLANES + h * 64);
     }
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) {
@@ -130,7 +131,7 @@ hipError_t launch_few(const MxGemmArgs& g, int waves, hipStream_t st) {
   static_assert(kMostFewWaves * BP * BQ * sizeof(float) <= 65536, "LDS without a raised limit");
   const int64_t tiles_q = g.offsets ? mx_most_tiles(g.T, g.experts, BQ) : (g.T + BQ - 1) / BQ;
   const int64_t tiles = (int64_t)((g.N + BP - 1) / BP) * tiles_q;
-  return launch_kernel(mx_few_kernel<FA, TP, TQ>, dim3((unsigned)tiles), dim3(64 * waves), waves * BP * BQ * sizeof(float), st, g);
+  return launch_mx_product(mx_few_kernel<FA, TP, TQ>, (unsigned)tiles, 64 * waves, waves * BP * BQ * sizeof(float), st, g);
 }
 
 }  // namespace

@@ -32,7 +32,8 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
 
 // (One place per thread: two took 0 to 20 % longer, four 10 to 60 % on small tensors.)
 template <int TYPE, int FORMAT, bool GATED>
-__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const void* x, int64_t stride, int64_t rows, int cols, MxOut out) {
+__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const void* x, int64_t stride, int64_t rows, int cols, uint8_t* codes, uint8_t* scales, void* values) {
+  const MxOut out{codes, scales, values};
   using T = typename MxElement<TYPE>::type;
   const int padded = (cols + 127) & ~127;
   const uint32_t per_row = (uint32_t)padded / 8;
@@ -56,15 +57,6 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const void* x, in
 }
 
 // ---- norm: h = x + residual, y = h * rsqrt(mean(h^2) + eps) * gamma
-
-struct NormArgs {
-  const void *x, *residual, *gamma;
-  void* residual_out;
-  MxOut out;
-  int64_t stride, rows;
-  int32_t cols;
-  float eps;
-};
 
 // Sum over LANES consecutive lanes (16, 32 or 64), in all of them.
 template <int LANES>
@@ -90,15 +82,17 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // workgroup are read twice (the second time mostly from the L2).  A place is read, and its residual written, by one thread, so
 // the new residual may lie where the old one, or x, was.  gamma is under way while the squares are added up.
 template <int TYPE, int FORMAT, int VECS, int LANES>
-__global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(NormArgs a) {
+__global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const void* residual, int64_t stride, int cols, float eps, const void* gamma_,
+                                                          void* residual_out, uint8_t* codes, uint8_t* scales, void* values, int64_t rows) {
+  const MxOut out{codes, scales, values};
   using T = typename MxElement<TYPE>::type;
   const int64_t row = LANES ? (int64_t)blockIdx.x * (256 / (LANES ? LANES : 1)) + threadIdx.x / (LANES ? LANES : 1) : blockIdx.x;
-  if (LANES && row >= a.rows) return;  // (all lanes of a row)
+  if (LANES && row >= rows) return;  // (all lanes of a row)
   const int place = LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x, threads = LANES ? LANES : blockDim.x;
-  const int cols = a.cols, padded = (cols + 127) & ~127;
-  const T* x = static_cast<const T*>(a.x) + row * a.stride;
-  const T* res = a.residual ? static_cast<const T*>(a.residual) + row * cols : nullptr;
-  const T* gamma = static_cast<const T*>(a.gamma);
+  const int padded = (cols + 127) & ~127;
+  const T* x = static_cast<const T*>(x_) + row * stride;
+  const T* res = residual ? static_cast<const T*>(residual) + row * cols : nullptr;
+  const T* gamma = static_cast<const T*>(gamma_);
   auto load = [&](int col, float (&h)[8]) {
     mx_load8<TYPE>(x + col, cols - col, h);
     if (res) {
@@ -114,10 +108,10 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(NormArgs a) {
     return s;
   };
   auto finish = [&](int col, float (&h)[8], float factor, const float (&g)[8]) {
-    if (a.residual_out && col < cols) mx_store8<TYPE>(static_cast<T*>(a.residual_out) + row * cols + col, cols - col, h);
+    if (residual_out && col < cols) mx_store8<TYPE>(static_cast<T*>(residual_out) + row * cols + col, cols - col, h);
 #pragma unroll
     for (int k = 0; k < 8; ++k) h[k] = gamma ? h[k] * factor * g[k] : h[k] * factor;
-    mx_put8<TYPE, FORMAT>(a.out, row, cols, padded, col, h);
+    mx_put8<TYPE, FORMAT>(out, row, cols, padded, col, h);
   };
   auto factor_of = [&](float mine) {
     float sum;
@@ -133,7 +127,7 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(NormArgs a) {
         sum = lanes_sum<16>((lane & 15) < waves ? parts[lane & 15] : 0.0f);
       }
     }
-    return 1.0f / sqrtf(sum / (float)cols + a.eps);
+    return 1.0f / sqrtf(sum / (float)cols + eps);
   };
   if constexpr (VECS > 0) {
     float h[VECS][8], g[VECS][8];
@@ -195,9 +189,10 @@ hipError_t quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t
     const int64_t n = rows - row < most ? rows - row : most;
     const hipError_t e = by_type(type, format, [&]<int TYPE, int FORMAT>() {
       using T = typename MxElement<TYPE>::type;
+      const MxOut to = out.from<T>(row, cols, format);
       const int64_t blocks = (n * (mx_padded(cols) / 8) + kThreads - 1) / kThreads;
       return launch_kernel(mx_quantize_kernel<TYPE, FORMAT, GATED>, dim3((unsigned)blocks), dim3(kThreads), 0, st,
-                           static_cast<const T*>(x) + row * stride, stride, n, (int)cols, out.from<T>(row, cols, format));
+                           static_cast<const T*>(x) + row * stride, stride, n, (int)cols, to.codes, to.scales, to.values);
     });
     if (e != hipSuccess) return e;
   }
@@ -228,7 +223,7 @@ hipError_t launch_mx_rmsnorm(const void* x, const void* residual, const void* ga
       using T = typename MxElement<TYPE>::type;
       const T* res = residual ? static_cast<const T*>(residual) + row * cols : nullptr;
       T* res_out = residual_out ? static_cast<T*>(residual_out) + row * cols : nullptr;
-      const NormArgs a{static_cast<const T*>(x) + row * stride, res, gamma, res_out, out.from<T>(row, cols, format), stride, n, (int32_t)cols, eps};
+      const MxOut to = out.from<T>(row, cols, format);
       const auto kern = lanes == 16   ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 16>
                         : lanes == 32 ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 32>
                         : lanes == 64 ? mx_rmsnorm_kernel<TYPE, FORMAT, 1, 64>
@@ -236,7 +231,8 @@ hipError_t launch_mx_rmsnorm(const void* x, const void* residual, const void* ga
                         : vecs == 2   ? mx_rmsnorm_kernel<TYPE, FORMAT, 2, 0>
                         : vecs == 4   ? mx_rmsnorm_kernel<TYPE, FORMAT, 4, 0>
                                       : mx_rmsnorm_kernel<TYPE, FORMAT, 0, 0>;
-      return launch_kernel(kern, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(threads), 0, st, a);
+      return launch_kernel(kern, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(threads), 0, st, static_cast<const T*>(x) + row * stride, res, stride, (int)cols, eps, gamma,
+                           res_out, to.codes, to.scales, to.values, n);
     });
     if (e != hipSuccess) return e;
   }

@@ -144,7 +144,8 @@ __device__ __forceinline__ void leave_by_quads(const MxGemmArgs& g, const mx_v16
 }
 
 template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
-__global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(MxGemmArgs g) {
+__global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_PARAMETERS) {
+  const MxGemmArgs g = HAGO_MX_GEMM_STRUCT;
   using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS>;
   constexpr int NW = Tile::NW, BP = Tile::BP, BQ = Tile::BQ, PLANES = Tile::PLANES, DATA = Tile::DATA, STAGE = Tile::STAGE;
   constexpr int GP = BP / 8, G = GP + PLANES * BQ / 8;   // loads of a stage: of P, in all
@@ -448,9 +449,7 @@ hipError_t launch_tile(const MxGemmArgs& g, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int64_t tiles_q = g.offsets ? mx_most_tiles(g.T, g.experts, Tile::BQ) : (g.T + Tile::BQ - 1) / Tile::BQ;
   const int64_t tiles = (int64_t)((g.N + Tile::BP - 1) / Tile::BP) * tiles_q;
-  MxGemmArgs a = g;
-  a.grid = (uint32_t)(Tile::STAYS && tiles > 256 * Tile::RESIDENT ? 256 * Tile::RESIDENT : tiles);
-  return launch_kernel(kern, dim3(a.grid), dim3(Tile::NT), Tile::LDS, st, a);
+  return launch_mx_product(kern, (unsigned)(Tile::STAYS && tiles > 256 * Tile::RESIDENT ? 256 * Tile::RESIDENT : tiles), Tile::NT, Tile::LDS, st, g);
 }
 
 }  // namespace
