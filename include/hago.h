@@ -425,11 +425,12 @@ typedef enum { HAGO_MX_FP4 = 0, HAGO_MX_FP8 = 1 } hago_mx_format;
 
 /*
  * The operators by rows.  x_t: HAGO_F32, HAGO_BF16 or HAGO_F16, the type of
- * every real tensor of the call; arithmetic is binary32.  x[rows, cols] may
- * have any row_stride (in elements) of at least its columns; all else is dense.
- * `values`, unless NULL, takes the values that the codes stand for, rounded to
- * x_t once, as [rows, cols]: the simulated quantization of the same numbers
- * (as hago_simquant_codes returns both).
+ * every real tensor of the call; arithmetic is binary32, the norm's sum and
+ * its root binary64.  x[rows, cols] may have any row_stride (in elements) of
+ * at least its columns; all else is dense.  `values`, unless NULL, takes the
+ * values that the codes stand for, rounded to x_t once, as [rows, cols]: the
+ * simulated quantization of the same numbers (hago_simquant_codes returns both
+ * too).
  *   hago_mx_quantize: codes of x.
  *   hago_mx_rmsnorm: h = x + residual (NULL: h = x), codes of
  *     y = h * rsqrt(mean(h^2) + eps) * gamma[col] (NULL: 1); residual_out,

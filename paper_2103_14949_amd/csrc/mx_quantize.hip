@@ -60,27 +60,45 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const void* x, in
 
 // Sum over LANES consecutive lanes (16, 32 or 64), in all of them.
 template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v) {
-  auto add = [&]<int CTRL>() { v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)); };
-  add.template operator()<0xB1>();   // quad_perm 1,0,3,2
-  add.template operator()<0x4E>();   // quad_perm 2,3,0,1
-  add.template operator()<0x141>();  // mirrored within eight lanes
-  add.template operator()<0x140>();  // mirrored within sixteen
-  // (a bit cast of a vector's element takes the first one, whichever is named: the elements are copied out)
-  const auto with = [&](const auto& swap) {
-    const auto s = swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v));
-    const uint32_t a = s[0], b = s[1];
-    v = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+__device__ __forceinline__ double lanes_sum(double v) {
+  const auto with = [&](const auto& exchange) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = exchange((uint32_t)b), hi = exchange((uint32_t)(b >> 32));
+    v += __builtin_bit_cast(double, hi << 32 | lo);
   };
-  if constexpr (LANES >= 32) with([](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane16_swap(a, b, false, false); });
-  if constexpr (LANES >= 64) with([](uint32_t a, uint32_t b) { return __builtin_amdgcn_permlane32_swap(a, b, false, false); });
+  auto dpp = [&]<int CTRL>() { with([](uint32_t d) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)d, CTRL, 0xf, 0xf, true); }); };
+  dpp.template operator()<0xB1>();   // quad_perm 1,0,3,2
+  dpp.template operator()<0x4E>();   // quad_perm 2,3,0,1
+  dpp.template operator()<0x141>();  // mirrored within eight lanes
+  dpp.template operator()<0x140>();  // mirrored within sixteen
+  // (of a swap of a register with a copy of it, one of the two results is what the other lanes had)
+  const bool odd16 = threadIdx.x & 16, odd32 = threadIdx.x & 32;
+  if constexpr (LANES >= 32)
+    with([&](uint32_t d) {
+      const auto s = __builtin_amdgcn_permlane16_swap(d, d, false, false);
+      const uint32_t even = s[0], odd = s[1];
+      return odd16 ? even : odd;
+    });
+  if constexpr (LANES >= 64)
+    with([&](uint32_t d) {
+      const auto s = __builtin_amdgcn_permlane32_swap(d, d, false, false);
+      const uint32_t even = s[0], odd = s[1];
+      return odd32 ? even : odd;
+    });
   return v;
+}
+
+// 1 / sqrt(v) to the last bits of binary64: the hardware's estimate and one step of Newton's.  0 of an infinity.
+__device__ __forceinline__ double inverse_root(double v) {
+  const double r = __builtin_amdgcn_rsq(v);
+  return r == 0.0 ? 0.0 : r * (1.5 - 0.5 * v * r * r);
 }
 
 // LANES lanes per row, 16 to 64 (rows of up to 512 columns, 256 / LANES rows per workgroup), or 0: one workgroup per row.  The row stays in registers,
 // VECS places of eight columns per thread.  VECS == 0: rows beyond the registers of a
 // workgroup are read twice (the second time mostly from the L2).  A place is read, and its residual written, by one thread, so
-// the new residual may lie where the old one, or x, was.  gamma is under way while the squares are added up.
+// the new residual may lie where the old one, or x, was.  gamma is under way while the squares are added up.  The sum and its
+// root are in 64 bits, and y is rounded to 32 once, from products in two parts: what y is rounded to next are codes, and an error in front of that moves some of them.
 template <int TYPE, int FORMAT, int VECS, int LANES>
 __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const void* residual, int64_t stride, int cols, float eps, const void* gamma_,
                                                           void* residual_out, uint8_t* codes, uint8_t* scales, void* values, int64_t rows) {
@@ -102,36 +120,41 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const 
       for (int k = 0; k < 8; ++k) h[k] += r[k];
     }
   };
-  auto square = [](const float (&h)[8], float s) {
+  auto square = [](const float (&h)[8], double s) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s = __builtin_fmaf(h[k], h[k], s);
+    for (int k = 0; k < 8; ++k) s = __builtin_fma((double)h[k], (double)h[k], s);
     return s;
   };
-  auto finish = [&](int col, float (&h)[8], float factor, const float (&g)[8]) {
+  auto finish = [&](int col, float (&h)[8], double factor, const float (&g)[8]) {
+    const float f = (float)factor, rest = (float)(factor - f);
     if (residual_out && col < cols) mx_store8<TYPE>(static_cast<T*>(residual_out) + row * cols + col, cols - col, h);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) h[k] = gamma ? h[k] * factor * g[k] : h[k] * factor;
+    for (int k = 0; k < 8; ++k) {
+      const float p = h[k] * f, e = __builtin_fmaf(h[k], rest, __builtin_fmaf(h[k], f, -p));
+      const float y = p * g[k];
+      h[k] = gamma ? y + __builtin_fmaf(e, g[k], __builtin_fmaf(p, g[k], -y)) : p + e;
+    }
     mx_put8<TYPE, FORMAT>(out, row, cols, padded, col, h);
   };
-  auto factor_of = [&](float mine) {
-    float sum;
+  auto factor_of = [&](double mine) {
+    double sum;
     if constexpr (LANES != 0) {
       sum = lanes_sum<LANES>(mine);
     } else {
-      __shared__ float parts[16];
+      __shared__ double parts[16];
       const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
       sum = lanes_sum<64>(mine);
       if (waves > 1) {
         if (lane == 0) parts[threadIdx.x >> 6] = sum;
         __syncthreads();
-        sum = lanes_sum<16>((lane & 15) < waves ? parts[lane & 15] : 0.0f);
+        sum = lanes_sum<16>((lane & 15) < waves ? parts[lane & 15] : 0.0);
       }
     }
-    return 1.0f / sqrtf(sum / (float)cols + eps);
+    return inverse_root(sum / (double)cols + (double)eps);
   };
   if constexpr (VECS > 0) {
     float h[VECS][8], g[VECS][8];
-    float sum = 0;
+    double sum = 0;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
       const int col = (place + i * threads) * 8;
@@ -147,19 +170,20 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const 
 #pragma unroll
     for (int i = 0; i < VECS; ++i)
       if ((place + i * threads) * 8 < padded) sum = square(h[i], sum);
-    const float factor = factor_of(sum);
+    const double factor = factor_of(sum);
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
       const int col = (place + i * threads) * 8;
       if (col < padded) finish(col, h[i], factor, g[i]);
     }
   } else {
-    float h[8], g[8], sum = 0;
+    float h[8], g[8];
+    double sum = 0;
     for (int col = place * 8; col < padded; col += threads * 8) {
       load(col, h);
       sum = square(h, sum);
     }
-    const float factor = factor_of(sum);
+    const double factor = factor_of(sum);
     for (int col = place * 8; col < padded; col += threads * 8) {
       load(col, h);
       if (gamma) mx_load8<TYPE>(gamma + col, cols - col, g);
