@@ -15,9 +15,13 @@ namespace hago {
 
 namespace {
 
-// What a call would take in a kernel, in us, from what this chip measured over a thousand dense and grouped products of 1 to 16384 rows,
-// 64 to 8192 features and k (the kernel it picks is 3 % slower than the fastest one on the average, 17 % in one of twenty).  A tile's time is `each` and
-// `step` per stage of 256 k, workgroups of a round on a CU share it, and alone it takes `alone` per stage, for it waits for its loads.
+// About what a call takes in a kernel, in us.  A tile's time is `each` and `step` per stage of 256 k, workgroups of a round on a CU share it, and
+// alone it takes `alone` per stage, for it waits for its loads.  The constants are fitted to 3700 measured dense and grouped products of 1 to 16384
+// rows, 64 to 8192 features and k, weights from memory and not from the last-level cache, to the times and to the choice, longer calls counting more: what the
+// rule picks is 2.3 % slower than the fastest kernel on the average (2.4 % on the quarter of the products that was left out of the fit), 13 % in one
+// of twenty.  Examples, 8192 rows through 8192 x 8192: 4-bit rows 276 us with 256 x 256 tiles, 356 with 128 x 128, 502 with 128 x 64; 8-bit rows 390 with
+// 256 x 256, 453 with 256 x 128, 618 with 128 x 64.  1024 rows through 4096 x 4096: 4-bit 28.3, 16.0, 17.4; 8-bit 37.9, 27.9, 22.1.
+// 300 rows there: 128 x 64 12.3 and 13.8, 64 x 64 10.3 and 12.5.
 struct MxShape {
   int bp, bq;      // features and rows of a tile
   int waves;       // of a workgroup with few rows; 0: operands through LDS
@@ -26,16 +30,16 @@ struct MxShape {
 };
 constexpr int kShapes = 13;
 constexpr MxShape kMxShapes[2][kShapes] = {
-    {{256, 256, 0, 0.00f, 6.23f, 0.82f, 1.21f, 0}, {128, 128, 0, 3.62f, 1.74f, 0.48f, 0.56f, 0}, {128, 64, 0, 3.66f, 0.93f, 0.54f, 0.42f, 0},
-     {64, 64, 0, 2.72f, 0.56f, 0.34f, 0.28f, 0}, {64, 32, 0, 2.86f, 0.74f, 0.29f, 0.21f, 0}, {16, 16, 4, 2.602f, 0.101f, 0.313f, 0.197f, 0.015f},
-     {16, 16, 8, 2.509f, 0.302f, 0.494f, 0.183f, 0.009f}, {32, 16, 2, 3.202f, 0.000f, 0.153f, 0.342f, 0.050f}, {32, 16, 4, 2.789f, 0.196f, 0.139f, 0.292f, 0.052f},
-     {32, 16, 8, 2.332f, 0.609f, 0.984f, 0.294f, 0.015f}, {32, 32, 16, 1.024f, 3.031f, 3.269f, 0.192f, 0.081f}, {16, 16, 16, 1.996f, 0.866f, 0.300f, 0.184f, 0.000f},
-     {32, 16, 16, 1.628f, 1.577f, 0.773f, 0.266f, 0.042f}},
-    {{256, 128, 0, 0.29f, 5.61f, 0.46f, 1.23f, 0}, {128, 128, 0, 1.69f, 3.96f, 0.31f, 0.82f, 0}, {128, 64, 0, 3.56f, 1.19f, 0.70f, 0.52f, 0},
-     {64, 64, 0, 2.65f, 0.75f, 0.47f, 0.34f, 0}, {64, 32, 0, 2.60f, 1.16f, 0.39f, 0.27f, 0}, {16, 16, 4, 2.657f, 0.028f, 0.302f, 0.239f, 0.093f},
-     {16, 16, 8, 2.526f, 0.252f, 0.565f, 0.223f, 0.090f}, {32, 16, 2, 3.043f, 0.000f, 0.300f, 0.383f, 0.112f}, {32, 16, 4, 2.858f, 0.136f, 0.462f, 0.345f, 0.108f},
-     {32, 16, 8, 2.458f, 0.559f, 0.910f, 0.337f, 0.073f}, {32, 32, 16, 0.760f, 3.036f, 3.549f, 0.301f, 0.146f}, {16, 16, 16, 2.056f, 0.844f, 0.696f, 0.230f, 0.054f},
-     {32, 16, 16, 1.591f, 1.627f, 1.162f, 0.310f, 0.112f}}};
+    {{256, 256, 0, 0.00f, 9.50f, 1.55f, 1.08f, 0}, {128, 128, 0, 5.04f, 1.42f, 0.67f, 0.40f, 0}, {128, 64, 0, 3.65f, 0.87f, 1.18f, 0.36f, 0},
+     {64, 64, 0, 2.85f, 0.52f, 0.67f, 0.23f, 0}, {64, 32, 0, 3.04f, 0.96f, 0.23f, 0.20f, 0}, {16, 16, 4, 2.807f, 0.018f, 0.352f, 0.225f, 0.000f},
+     {16, 16, 8, 2.665f, 0.297f, 0.072f, 0.196f, 0.000f}, {32, 16, 2, 3.168f, 0.000f, 0.226f, 0.408f, 0.000f}, {32, 16, 4, 3.060f, 0.098f, 0.003f, 0.336f, 0.056f},
+     {32, 16, 8, 2.466f, 0.731f, 0.035f, 0.341f, 0.008f}, {32, 32, 16, 1.065f, 3.083f, 0.248f, 0.243f, 0.060f}, {16, 16, 16, 2.199f, 0.869f, 0.066f, 0.184f, 0.000f},
+     {32, 16, 16, 1.678f, 1.752f, 0.027f, 0.292f, 0.027f}},
+    {{256, 256, 0, 0.00f, 5.41f, 2.32f, 1.96f, 0}, {256, 128, 0, 0.00f, 5.33f, 1.86f, 1.39f, 0}, {128, 64, 0, 3.65f, 1.31f, 0.88f, 0.52f, 0},
+     {64, 64, 0, 2.75f, 0.59f, 0.79f, 0.38f, 0}, {64, 32, 0, 2.68f, 1.97f, 0.32f, 0.22f, 0}, {16, 16, 4, 2.622f, 0.030f, 0.537f, 0.238f, 0.053f},
+     {16, 16, 8, 2.491f, 0.247f, 0.668f, 0.218f, 0.052f}, {32, 16, 2, 3.148f, 0.010f, 0.367f, 0.366f, 0.089f}, {32, 16, 4, 3.125f, 0.116f, 0.011f, 0.315f, 0.087f},
+     {32, 16, 8, 2.380f, 0.596f, 1.300f, 0.322f, 0.066f}, {32, 32, 16, 1.120f, 3.184f, 1.354f, 0.261f, 0.086f}, {16, 16, 16, 2.056f, 0.864f, 1.123f, 0.196f, 0.052f},
+     {32, 16, 16, 1.600f, 1.544f, 1.917f, 0.296f, 0.139f}}};
 
 int pick_shape(const MxGemmArgs& g, int a_format) {
   const double k = (double)mx_padded(g.K);
@@ -63,11 +67,11 @@ int pick_shape(const MxGemmArgs& g, int a_format) {
 template <int FA>
 hipError_t launch_shape(const MxGemmArgs& g, int shape, hipStream_t st) {
   switch (shape) {
-    case 0: return FA == kMxFp4 ? launch_tile<kMxFp4, 2, 4, 4, 2, 2>(g, st) : launch_tile<kMxFp8, 4, 2, 2, 2, 2>(g, st);
-    case 1: return launch_tile<FA, 2, 2, 2, 2, 2>(g, st);
-    case 2: return launch_tile<FA, 2, 2, 2, 1, 2>(g, st);
-    case 3: return launch_tile<FA, 2, 2, 1, 1, 2>(g, st);
-    case 4: return launch_tile<FA, 2, 1, 1, 1, 4>(g, st);
+    case 0: return FA == kMxFp4 ? launch_tile<kMxFp4, 2, 4, 4, 2, 2, 256>(g, st) : launch_tile<kMxFp8, 2, 4, 4, 2, 3, 128>(g, st);
+    case 1: return FA == kMxFp4 ? launch_tile<kMxFp4, 2, 2, 2, 2, 2, 256>(g, st) : launch_tile<kMxFp8, 4, 2, 2, 2, 2, 256>(g, st);
+    case 2: return launch_tile<FA, 2, 2, 2, 1, 2, 256>(g, st);
+    case 3: return launch_tile<FA, 2, 2, 1, 1, 2, 256>(g, st);
+    case 4: return launch_tile<FA, 2, 1, 1, 1, 4, 256>(g, st);
     case 5: case 6: case 11: return launch_few<FA, 1, 1>(g, kMxShapes[FA][shape].waves, st);
     case 10: return launch_few<FA, 2, 2>(g, kMxShapes[FA][shape].waves, st);
     default: return launch_few<FA, 2, 1>(g, kMxShapes[FA][shape].waves, st);

@@ -3,7 +3,7 @@
 //
 // A lane takes eight consecutive columns, a quad of lanes a block of 32: the block's largest magnitude takes two lane exchanges, and
 // the codes leave as 4 or 8 consecutive bytes per lane.  All three move bytes and little else: 8192 x 8192 fp32 to 4 bits with values in 100 us, norm
-// of 8192 x 4096 bf16 with residual and values in 50, activation of 16384 x 4096 bf16 with values in 84 (5.7, 6.1 and 5.6 TB/s; a copy of 1 GiB 5.0).
+// of 8192 x 4096 bf16 with residual and values in 51, activation of 16384 x 4096 bf16 with values in 84 (5.7, 5.9 and 5.6 TB/s; a copy of 1 GiB 5.0).
 #include "mx_device.h"
 
 namespace hago {

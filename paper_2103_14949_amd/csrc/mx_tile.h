@@ -1,14 +1,25 @@
 // Microscaled products on tiles whose operands stream from memory straight into LDS.
 //
-// D[i][j] = sum_k P[i][k] Q[j][k], P = weights (i = feature, contiguous in the result), Q = activations.  A stage is 256 k of a tile's
-// rows: 128 bytes of a row of 4-bit codes (whole lines), two planes of 128 bytes of one of 8-bit codes, and 8 scale bytes a row.
-// SLOTS slots of LDS hold a stage each.  A stage has four groups of 64 k, one matrix instruction per 32 x 32 block each; fragments
+// D[i][j] = sum_k P[i][k] Q[j][k], P = weights (i = feature, contiguous in the result), Q = activations.  A stage is KB = 256 or 128 k of a
+// tile's rows: KB / 2 bytes of a row of 4-bit codes (256: whole lines), planes of 128 bytes of one of 8-bit codes, and KB / 32 scale bytes a
+// row.  SLOTS slots of LDS hold a stage each.  A stage has groups of 64 k, one matrix instruction per 32 x 32 block each; fragments
 // are double-buffered by groups, so that before its last group a stage has been read completely: there lies the one barrier of a stage,
 // behind it the loads of a later stage go out into the slot just read, and the next group's fragments come from the next slot.
 //
-// LDS.  A load of a wavefront fills 1 KB: 8 rows of 128 bytes, the 16-byte chunks of a row permuted by bits 1 to 3 of the row
-// (swz in qgemm_stream.h), on the global side, so that fragments are read at the full rate.  Scales lie as [row][8 bytes]; a lane takes a dword for half a stage and shifts
-// its half's byte of either pair down, so that one byte select serves both halves of the wavefront.
+// What bounds it.  The matrix instructions alone run at 6800 (4-bit rows) and 4200 TFLOP/s (8-bit rows) on such codes; 8192 rows through
+// 8192 x 8192 take 265 us (4150) and 390 us (2820).  The matrix unit is busy for 56 to 62 % of the cycles, at 1.6 GHz of 2.4: power sets the clock,
+// and the fragments' reads of LDS fill the rest.  So the tile is the one with the fewest bytes of LDS per instruction that the registers hold, 256 x 256 by
+// eight wavefronts of 128 x 64.  8-bit rows leave no room for two stages of 256 k of it (197 KB); three of 128 k fit (150 KB): 390 us, and 453 with
+// 256 x 128 tiles of two stages of 256 k.  4-bit rows with stages of 128 k in four slots take 331 us instead of 276, 128 x 128 tiles 512 instead of 356:
+// a row's half line is fetched twice and there are twice the barriers.  Other forms: four wavefronts of 128 x 128 with 4-bit rows 283 us against 260, a
+// higher priority for wavefronts in matrix instructions no difference.
+//
+// A workgroup stays for several tiles where the loads of the next one's first stages fit behind the last one's (Tile::STAYS).  Results leave
+// from the registers by pieces of whole 64 bytes that quads of lanes exchange, and by LDS where a wavefront has one 32-feature block only.
+//
+// LDS.  A load of a wavefront fills 1 KB: 8 rows of 128 bytes or 16 of 64, the 16-byte chunks of a row permuted by bits of the row
+// (swz in qgemm_stream.h), on the global side, so that fragments are read at the full rate.  Scales lie as [row][KB / 32 bytes]; a lane takes a
+// dword for 128 k and shifts its half's byte of either pair down, so that one byte select serves both halves of the wavefront.
 //
 // Out of range.  Loads go through descriptors of the tile's own rows (64-bit base, so tensors have any size), and lanes whose row or k
 // lies outside get an offset beyond: zeros, code and scale, whose products are zero.
@@ -38,12 +49,13 @@ __device__ __forceinline__ void mx_dma4(v4i rsrc, uint32_t lds_addr, uint32_t vo
                : "memory", "m0", "scc");
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB>
 struct MxTile {
   static constexpr int NW = WP * WQ, NT = 64 * NW;
   static constexpr int BP = WP * TP * 32, BQ = WQ * TQ * 32;
-  static constexpr int PLANES = FA == kMxFp8 ? 2 : 1;
-  static constexpr int DATA = (BP + PLANES * BQ) * 128, STAGE = DATA + (BP + BQ) * 8;
+  static constexpr int PB = KB / 2, SB = KB / 32;  // bytes of a row of weights and of scales in a stage
+  static constexpr int QB = FA == kMxFp8 ? 128 : PB, PLANES = FA == kMxFp8 ? KB / 128 : 1;  // of a plane's row of activations
+  static constexpr int DATA = BP * PB + PLANES * BQ * QB, STAGE = DATA + (BP + BQ) * SB;
   // rows leave from the registers where a wavefront has pairs of 32-feature blocks, by LDS otherwise
   static constexpr bool BY_LDS = TP % 2 != 0;
   static constexpr int PITCH = TP * 128 + 16;  // bytes of a result row in LDS, at most
@@ -143,16 +155,18 @@ __device__ __forceinline__ void leave_by_quads(const MxGemmArgs& g, const mx_v16
     }
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB>
 __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_PARAMETERS) {
   const MxGemmArgs g = HAGO_MX_GEMM_STRUCT;
-  using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS>;
+  using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS, KB>;
   constexpr int NW = Tile::NW, BP = Tile::BP, BQ = Tile::BQ, PLANES = Tile::PLANES, DATA = Tile::DATA, STAGE = Tile::STAGE;
-  constexpr int GP = BP / 8, G = GP + PLANES * BQ / 8;   // loads of a stage: of P, in all
-  constexpr int L = G / NW;                              // a wavefront issues loads wave, wave + NW, ...
-  static_assert(GP % NW == 0 && G % NW == 0 && NW % 2 == 0, "a load's operand is the same in every wavefront");
-  constexpr int GS = (BP + BQ) / 32, LS = (GS + NW - 1) / NW;  // loads of scales (some twice where NW does not divide them)
-  constexpr int NM = TP * TQ;
+  constexpr int PB = Tile::PB, QB = Tile::QB, SB = Tile::SB;
+  constexpr int RP = 1024 / PB, RQ = 1024 / QB, RS = 256 / SB;   // rows of a load
+  constexpr int GP = BP / RP, G = GP + PLANES * BQ / RQ;         // loads of a stage: of P, in all
+  constexpr int L = G / NW;                                      // a wavefront issues loads wave, wave + NW, ...
+  static_assert(GP % NW == 0 && G % NW == 0 && NW % 2 == 0 && BP % RS == 0, "a load's operand is the same in every wavefront");
+  constexpr int GS = (BP + BQ) / RS, LS = (GS + NW - 1) / NW;    // loads of scales (some twice where NW does not divide them)
+  constexpr int NM = TP * TQ, GROUPS = KB / 64;
 
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
@@ -163,7 +177,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   const uint32_t wbytes = (uint32_t)padded / 2, abytes = FA == kMxFp4 ? wbytes : (uint32_t)padded, sbytes = (uint32_t)padded / 32;
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)smem, wave_lds = lds0 + (uint32_t)wave * 1024;
   // (of a workgroup that stays, whole rounds of the slots: its last stage may hold nothing)
-  const int KT = (padded + 255) / 256, stages = Tile::STAYS ? (KT + SLOTS - 1) / SLOTS * SLOTS : KT;
+  const int KT = (padded + KB - 1) / KB, stages = Tile::STAYS ? (KT + SLOTS - 1) / SLOTS * SLOTS : KT;
 
   const int tiles_p = (g.N + BP - 1) / BP;
   const MxGroups<BQ> groups(g);
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   // The rows of a tile's activations that this lane loads, of those the descriptors begin with; negative: none.  Both planes of a row are the same
   // lane's, so one of PLANES loads stands for all.
   constexpr int LQ = (G - GP) / NW / PLANES;
-  const int lrow = lane / 8;
+  const int prow_of = lane / (PB / 16), qrow_of = lane / (QB / 16);  // the lane's row of a load
   struct Picked {
     int q[LQ], s[LS];
   };
@@ -192,10 +206,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
     auto row_of = [&](int r) { return r < nq ? (g.index ? mx_row_of(g, at.rows.row + r) : r) : -1; };
     Picked p;
 #pragma unroll
-    for (int d = 0; d < LQ; ++d) p.q[d] = row_of((wave + NW * d) * 8 + lrow);
+    for (int d = 0; d < LQ; ++d) p.q[d] = row_of((wave + NW * d) * RQ + qrow_of);
 #pragma unroll
     for (int d = 0; d < LS; ++d) {
-      const int v = (wave + NW * d) % GS * 32 + lane / 2;
+      const int v = (wave + NW * d) % GS * RS + lane / (SB / 4);
       p.s[d] = v >= BP ? row_of(v - BP) : at.p0 + v < g.N ? v : -1;
     }
     return p;
@@ -203,7 +217,11 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
 
   // A tile's descriptors, and the lane's byte offset of every load: its row's start and its chunk of a stage (the chunk is the same in
   // every load, since every load of a wavefront has the wavefront's parity).
-  const uint32_t lck = (uint32_t)(((lane % 8) ^ swz<128>((wave & 1) * 8 + lrow)) * 16);
+  auto chunk_of = [&](auto bytes, int row) {
+    constexpr int B = decltype(bytes)::value;
+    return (uint32_t)(((lane % (B / 16)) ^ swz<B>(B == 128 ? (wave & 1) * 8 + row : row)) * 16);
+  };
+  const uint32_t pck = chunk_of(template_int<PB>{}, prow_of), qck = chunk_of(template_int<QB>{}, qrow_of), sck = (uint32_t)(lane % (SB / 4)) * 4;
   v4i rs_w, rs_ws, rs_a, rs_as;
   uint32_t voff[L], soff[LS];
   auto bind = [&](const Place& at, const Picked& picked) {
@@ -215,22 +233,22 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
 #pragma unroll
     for (int d = 0; d < L; ++d) {
       if (d < GP / NW) {
-        const int r = (wave + NW * d) * 8 + lrow;
-        voff[d] = r < np ? (uint32_t)r * wbytes + lck : kOob;
+        const int r = (wave + NW * d) * RP + prow_of;
+        voff[d] = r < np ? (uint32_t)r * wbytes + pck : kOob;
       } else {
         constexpr int kPlane = LQ;  // loads of a plane
         const int e = d - GP / NW, plane = e / kPlane, r = picked.q[e % kPlane];
-        voff[d] = r >= 0 ? (uint32_t)r * abytes + lck + (uint32_t)plane * 128 : kOob;
+        voff[d] = r >= 0 ? (uint32_t)r * abytes + qck + (uint32_t)plane * QB : kOob;
       }
     }
 #pragma unroll
-    for (int d = 0; d < LS; ++d) soff[d] = picked.s[d] >= 0 ? (uint32_t)picked.s[d] * sbytes + (uint32_t)(lane % 2) * 4 : kOob;
+    for (int d = 0; d < LS; ++d) soff[d] = picked.s[d] >= 0 ? (uint32_t)picked.s[d] * sbytes + sck : kOob;
   };
   constexpr int ISSUES = L + LS;
   // loads lo .. hi - 1 of a stage
   auto issue = [&](int stage, auto slot, auto lo, auto hi) {
     constexpr int base = decltype(slot)::value * STAGE;
-    const uint32_t kp = (uint32_t)stage * 128, kq = kp * PLANES, ks = (uint32_t)stage * 8;
+    const uint32_t kp = (uint32_t)stage * PB, kq = (uint32_t)stage * (QB * PLANES), ks = (uint32_t)stage * SB;
     const bool there = stage < KT;
     [&]<int... I>(std::integer_sequence<int, I...>) {
       ([&] {
@@ -238,80 +256,80 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
         if constexpr (d < L) {
           constexpr bool isq = d >= GP / NW;
           constexpr int plane = isq && PLANES > 1 ? (d - GP / NW) / LQ : 0;
-          const uint32_t at = (isq ? kq + plane * 128 : kp) + lck, end = isq ? abytes : wbytes;
+          const uint32_t at = isq ? kq + plane * QB + qck : kp + pck, end = isq ? abytes : wbytes;
           mx_dma16<base + NW * d * 1024>(isq ? rs_a : rs_w, wave_lds, at < end ? voff[d] : kOob, there ? (isq ? kq : kp) : 0);
         } else {
           constexpr int s = d - L;
           const int grp = (wave + NW * s) % GS;
-          mx_dma4<base + DATA>(grp >= BP / 32 ? rs_as : rs_ws, lds0 + (uint32_t)grp * 256, ks + (uint32_t)(lane % 2) * 4 < sbytes ? soff[s] : kOob, there ? ks : 0);
+          mx_dma4<base + DATA>(grp >= BP / RS ? rs_as : rs_ws, lds0 + (uint32_t)grp * 256, ks + sck < sbytes ? soff[s] : kOob, there ? ks : 0);
         }
       }(), ...);
     }(std::make_integer_sequence<int, decltype(hi)::value - decltype(lo)::value>{});
   };
-  static_assert(PLANES == 1 || (BQ / 8) % NW == 0, "a load's plane is the same in every wavefront");
+  static_assert(PLANES == 1 || (BQ / RQ) % NW == 0, "a load's plane is the same in every wavefront");
   template_int<0> i0;
 
   // fragment addresses inside a stage
   const int frow = lane & 31;
-  auto chunk_at = [&](int c) { return (c ^ swz<128>(frow & 15)) * 16; };
+  auto chunk_at = [&](auto bytes, int c) { return (c ^ swz<decltype(bytes)::value>(frow & 15)) * 16; };
+  template_int<PB> pb;
+  template_int<QB> qb;
   const int prow = wp * TP * 32 + frow, qrow = wq * TQ * 32 + frow;
-  int pa[4], qa[PLANES * 4];
+  constexpr int PIECES = FA == kMxFp8 ? 2 : 1;  // 16-byte pieces of a fragment of activations
+  int pa[GROUPS], qa[PIECES * GROUPS];
 #pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    pa[h] = prow * 128 + chunk_at(2 * h + half);
+  for (int h = 0; h < GROUPS; ++h) {
+    pa[h] = prow * PB + chunk_at(pb, 2 * h + half);
     if constexpr (FA == kMxFp4) {
-      qa[h] = (BP + qrow) * 128 + chunk_at(2 * h + half);
+      qa[h] = BP * PB + qrow * QB + chunk_at(qb, 2 * h + half);
     } else {
-      qa[2 * h] = (BP + (h / 2) * BQ + qrow) * 128 + chunk_at(4 * (h % 2) + half);
-      qa[2 * h + 1] = (BP + (h / 2) * BQ + qrow) * 128 + chunk_at(4 * (h % 2) + 2 + half);
+      qa[2 * h] = BP * PB + ((h / 2) * BQ + qrow) * QB + chunk_at(qb, 4 * (h % 2) + half);
+      qa[2 * h + 1] = BP * PB + ((h / 2) * BQ + qrow) * QB + chunk_at(qb, 4 * (h % 2) + 2 + half);
     }
   }
-  const int psa = DATA + prow * 8, qsa = DATA + (BP + qrow) * 8, shift = 8 * half;
-  constexpr int kFrag = 32 * 128;
-  mx_v4i pf[2][TP], qf[2][TQ * PLANES];
-  uint32_t sc[2][TP + TQ];  // scales of the first and of the second half of a stage
+  const int psa = DATA + prow * SB, qsa = DATA + (BP + qrow) * SB, shift = 8 * half;
+  mx_v4i pf[2][TP], qf[2][TQ * PIECES];
+  uint32_t sc[TP + TQ], sc_next[TP + TQ];  // scales of 128 k; the next ones as they are read
   // read r of the NR of a group's operands, activations first
-  constexpr int NR = TQ * PLANES + TP;
+  constexpr int NR = TQ * PIECES + TP;
   auto read = [&](const uint8_t* base, auto set, auto group, int r) {
     constexpr int S = decltype(set)::value, H = decltype(group)::value;
-    if (r < TQ * PLANES) qf[S][r] = *reinterpret_cast<const mx_v4i*>(base + qa[PLANES * H + r % PLANES] + (r / PLANES) * kFrag);
-    else pf[S][r - TQ * PLANES] = *reinterpret_cast<const mx_v4i*>(base + pa[H] + (r - TQ * PLANES) * kFrag);
+    if (r < TQ * PIECES) qf[S][r] = *reinterpret_cast<const mx_v4i*>(base + qa[PIECES * H + r % PIECES] + (r / PIECES) * 32 * QB);
+    else pf[S][r - TQ * PIECES] = *reinterpret_cast<const mx_v4i*>(base + pa[H] + (r - TQ * PIECES) * 32 * PB);
   };
-  auto read_scale = [&](const uint8_t* base, auto part, int r) {
-    constexpr int S = decltype(part)::value;
-    sc[S][r] = *reinterpret_cast<const uint32_t*>(base + (r < TP ? psa + r * 256 : qsa + (r - TP) * 256) + 4 * S);
+  auto read_scale = [&](const uint8_t* base, int part, int r) {
+    sc_next[r] = *reinterpret_cast<const uint32_t*>(base + (r < TP ? psa + r * 32 * SB : qsa + (r - TP) * 32 * SB) + 4 * part);
   };
-  auto shift_scales = [&](auto part) {
-    constexpr int S = decltype(part)::value;
+  auto shift_scales = [&] {
 #pragma unroll
-    for (int r = 0; r < TP + TQ; ++r) sc[S][r] >>= shift;
+    for (int r = 0; r < TP + TQ; ++r) sc[r] = sc_next[r] >> shift;
   };
   // Group H of a stage: multiply its set of fragments, behind the instructions go the reads of the next group's set (from `next`) and of
-  // the next half's scales in front of it, and in the last group the loads of stage `dma_stage`.
+  // the next 128 k's scales in front of them, and in the last group the loads of stage `dma_stage`.
   auto multiply = [&](mx_v16f (&acc)[TP][TQ], auto hconst, const uint8_t* next, int dma_stage, auto ring) {
     constexpr int H = decltype(hconst)::value, S = H & 1;
     constexpr int reads = NR + (H % 2 ? TP + TQ : 0), each = (reads + NM - 1) / NM > 2 ? (reads + NM - 1) / NM : 2;
     [&]<int... Mi>(std::integer_sequence<int, Mi...>) {
       ([&] {
         constexpr int m = Mi, j = m / TP, i = m % TP;
-        const mx_v4i p4 = pf[S][i], q4 = qf[S][j * PLANES], q5 = qf[S][j * PLANES + PLANES - 1];
+        const mx_v4i p4 = pf[S][i], q4 = qf[S][j * PIECES], q5 = qf[S][j * PIECES + PIECES - 1];
         const mx_v8i p = __builtin_shufflevector(p4, p4, 0, 1, 2, 3, -1, -1, -1, -1);
         mx_v8i q;
         if constexpr (FA == kMxFp4) q = __builtin_shufflevector(q4, q4, 0, 1, 2, 3, -1, -1, -1, -1);
         else q = __builtin_shufflevector(q4, q5, 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 2 * (H % 2), (int)sc[H / 2][i],
-                                                                    2 * (H % 2), (int)sc[H / 2][TP + j]);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 2 * (H % 2), (int)sc[i],
+                                                                    2 * (H % 2), (int)sc[TP + j]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = each * m; r < each * m + each && r < reads; ++r) {
-          if (r < NR) read(next, template_int<(S ^ 1)>{}, template_int<(H + 1) % 4>{}, r);
-          else read_scale(next, template_int<(H / 2 ^ 1)>{}, r - NR);
+          if (r < NR) read(next, template_int<(S ^ 1)>{}, template_int<(H + 1) % GROUPS>{}, r);
+          else read_scale(next, (H + 1) % GROUPS / 2, r - NR);
         }
-        if constexpr (H == 3) issue(dma_stage, ring, template_int<m * ISSUES / NM>{}, template_int<(m + 1) * ISSUES / NM>{});
+        if constexpr (H == GROUPS - 1) issue(dma_stage, ring, template_int<m * ISSUES / NM>{}, template_int<(m + 1) * ISSUES / NM>{});
         __builtin_amdgcn_sched_barrier(0);
       }(), ...);
     }(std::make_integer_sequence<int, NM>{});
-    if constexpr (H % 2 != 0) shift_scales(template_int<(H / 2 ^ 1)>{});
+    if constexpr (H % 2 != 0) shift_scales();
   };
   constexpr int kStores16 = TQ * TP / 2 * 4, kStores32 = 2 * kStores16;
   int stores = 0;  // of the last tile's results, behind the loads of this one's first two stages
@@ -331,11 +349,9 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
     constexpr int R = decltype(ring)::value;
     const uint8_t* here = smem + R * STAGE;
     const uint8_t* other = smem + (R + 1) % SLOTS * STAGE;
-    multiply(acc, template_int<0>{}, here, 0, ring);
-    multiply(acc, template_int<1>{}, here, 0, ring);
-    multiply(acc, template_int<2>{}, here, 0, ring);
+    [&]<int... H>(std::integer_sequence<int, H...>) { (multiply(acc, template_int<H>{}, here, 0, ring), ...); }(std::make_integer_sequence<int, GROUPS - 1>{});
     meet(kt);
-    multiply(acc, template_int<3>{}, other, fetched(kt), ring);
+    multiply(acc, template_int<GROUPS - 1>{}, other, fetched(kt), ring);
   };
   // a stage of which nothing is this wavefront's
   auto idle_stage = [&](int kt, auto ring) {
@@ -414,8 +430,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
 #pragma unroll
       for (int r = 0; r < NR; ++r) read(smem, i0, i0, r);
 #pragma unroll
-      for (int r = 0; r < TP + TQ; ++r) read_scale(smem, i0, r);
-      shift_scales(i0);
+      for (int r = 0; r < TP + TQ; ++r) read_scale(smem, 0, r);
+      shift_scales();
       auto work = [&](int kt, auto ring) { stage_body(acc, kt, ring); };
       for (int kt = 0; kt < KT; kt += SLOTS) {
         bind_next(kt);
@@ -440,10 +456,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may be on its way into LDS that is given back)
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB>
 hipError_t launch_tile(const MxGemmArgs& g, hipStream_t st) {
-  using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS>;
-  const auto kern = mx_tile_kernel<FA, WP, WQ, TP, TQ, SLOTS>;
+  using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS, KB>;
+  const auto kern = mx_tile_kernel<FA, WP, WQ, TP, TQ, SLOTS, KB>;
   static std::atomic<uint64_t> attr_set{0};  // the devices whose dynamic-LDS limit is raised
   const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), Tile::LDS, attr_set);
   if (e != hipSuccess) return e;

@@ -22,6 +22,6 @@ def test_a_refused_launch_is_reported_once(lines):
 @pytest.mark.parametrize("name,kernel", [
     ("quantize", "mx_quantize_kernel<1, 0, false>"), ("silu_mul", "mx_quantize_kernel<0, 1, true>"),
     ("rmsnorm", "mx_rmsnorm_kernel<2, 1, 1, 0>"), ("rmsnorm short", "mx_rmsnorm_kernel<0, 1, 1, 16>"),
-    ("dense few", "mx_few_kernel<1"), ("dense large", "mx_tile_kernel<0, 2, 4, 4, 2"), ("grouped", "mx_tile_kernel<1, 4, 2, 2, 2")])
+    ("dense few", "mx_few_kernel<1"), ("dense large", "mx_tile_kernel<0, 2, 4, 4, 2"), ("grouped", "mx_tile_kernel<1, 2, 4, 4, 2, 3")])
 def test_which_kernel_serves_a_call(lines, name, kernel):
     assert kernel in lines[name], lines[name]
