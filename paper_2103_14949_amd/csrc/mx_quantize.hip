@@ -27,7 +27,7 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
   const float r = __builtin_amdgcn_rcpf(d * kDown);
   const float q = (c * kDown) * r;
   const float s = __builtin_fmaf(__builtin_fmaf(-q, d, c) * kDown, r, q);
-  return (g < kLeast ? 0.0f : g > 1e30f ? g : s) * u;
+  return (g < kLeast ? 0.0f : g <= 1e30f ? s : g) * u;  // (the comparisons fail for a NaN, which is g itself)
 }
 
 // (One place per thread: two took 0 to 20 % longer, four 10 to 60 % on small tensors.)
