@@ -49,3 +49,17 @@ def test_a_gate_or_an_up_that_is_no_number_spoils_its_block_alone(name, fmt):
             x[row, cols + at] = up
         spoiled.append((row, at // 32))
     check(x, fmt, spoiled)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_gates_of_every_exponent(name, fmt):
+    """A row of gates for every exponent whose half is a normal number, of either sign, times ups that bring the products between 2^-10 and 2^10."""
+    gen = torch.Generator().manual_seed(5)
+    exponents = range(-125, 6)
+    rows = []
+    for e in exponents:
+        gate = torch.ldexp(1 + torch.rand(96, generator=gen), torch.tensor(e)) * torch.where(torch.rand(96, generator=gen) < 0.5, -1.0, 1.0)
+        up = torch.ldexp(1 + torch.rand(96, generator=gen), torch.tensor(min(-e, 120)))
+        rows.append(torch.cat([gate, up]))
+    check(torch.stack(rows).to(t.TYPES[name]), fmt)
