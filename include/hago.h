@@ -438,8 +438,10 @@ typedef enum { HAGO_MX_FP4 = 0, HAGO_MX_FP8 = 1 } hago_mx_format;
  *     rounding).  It may be residual itself, or x itself where
  *     row_stride == cols.
  *   hago_mx_silu_mul: x[rows, 2 cols]; codes of g / (1 + exp(-g)) * u with g
- *     the first cols columns of a row and u the others (g / (1 + exp(-g))
- *     within a few units of the last place, 0 for g below -88.72).
+ *     the first cols columns of a row and u the others, within a few units of
+ *     the last place of binary32 (of a product far below g's own size too; an
+ *     infinite g has what the formula makes of it: g * u, or NaN where it is
+ *     negative).
  * Errors: NULL (x, codes or scales), SHAPE (negative or beyond 2^31 - 129
  * columns or 2^62 elements, row_stride below the columns), DTYPE (x_t), PARAM
  * (format; eps negative or not finite; codes, scales misaligned, or a real

@@ -63,3 +63,28 @@ def test_gates_of_every_exponent(name, fmt):
         up = torch.ldexp(1 + torch.rand(96, generator=gen), torch.tensor(min(-e, 120)))
         rows.append(torch.cat([gate, up]))
     check(torch.stack(rows).to(t.TYPES[name]), fmt)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_gates_far_below_zero(name, fmt):
+    """Gates from -60 on down, times the largest ups, as long as the products are normal numbers; each with its own small neighbours and with
+    neighbours that leave it a zero; and the last finite one."""
+    gen = torch.Generator().manual_seed(6)
+    rows = []
+    for g in [*range(-60, -172, -2), -79.75, -80.5, -88.5, -88.75, -103.5]:
+        gate = torch.full((64,), float(g))
+        up = torch.ldexp(1 + torch.rand(64, generator=gen), torch.tensor(126)) * torch.where(torch.rand(64, generator=gen) < 0.5, -1.0, 1.0)
+        gate[32] = 1.0
+        rows.append(torch.cat([gate, up]))
+    x = torch.stack(rows).to(t.TYPES[name])
+    x[-1, 40], x[-1, 41], x[-1, 42] = -1e4, torch.finfo(t.TYPES[name]).min, -1000.0
+    check(x, fmt)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_a_gate_of_minus_infinity_is_no_number(fmt):
+    """By the formula: minus infinity by infinity."""
+    x = torch.randn(3, 200, generator=torch.Generator().manual_seed(7))
+    x[1, 5] = -float("inf")
+    check(x, fmt, [(1, 0)])
