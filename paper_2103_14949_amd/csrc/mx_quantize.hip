@@ -143,13 +143,18 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const 
     return s;
   };
   auto finish = [&](int col, float (&h)[8], double factor, const float (&g)[8]) {
-    const float f = (float)factor, rest = (float)(factor - f);
     if (residual_out && col < cols) mx_store8<TYPE>(static_cast<T*>(residual_out) + row * cols + col, cols - col, h);
+    if (factor > 0x1p-100 && factor < 0x1p100) {
+      const float f = (float)factor, rest = (float)(factor - f);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float p = h[k] * f, e = __builtin_fmaf(h[k], rest, __builtin_fmaf(h[k], f, -p));
-      const float y = p * g[k];
-      h[k] = gamma ? y + __builtin_fmaf(e, g[k], __builtin_fmaf(p, g[k], -y)) : p + e;
+      for (int k = 0; k < 8; ++k) {
+        const float p = h[k] * f, e = __builtin_fmaf(h[k], rest, __builtin_fmaf(h[k], f, -p));
+        const float y = p * g[k];
+        h[k] = gamma ? y + __builtin_fmaf(e, g[k], __builtin_fmaf(p, g[k], -y)) : p + e;
+      }
+    } else {  // (rows at the ends of binary32, where the factor or its second part is no normal number of it, and rows that have no factor)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) h[k] = (float)((double)h[k] * factor * (gamma ? (double)g[k] : 1.0));
     }
     mx_put8<TYPE, FORMAT>(out, row, cols, padded, col, h);
   };
