@@ -154,7 +154,7 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const 
       }
     } else {  // (rows at the ends of binary32, where the factor or its second part is no normal number of it, and rows that have no factor)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) h[k] = (float)((double)h[k] * factor * (gamma ? (double)g[k] : 1.0));
+      for (int k = 0; k < 8; ++k) h[k] = col + k < cols ? (float)((double)h[k] * factor * (gamma ? (double)g[k] : 1.0)) : 0.0f;
     }
     mx_put8<TYPE, FORMAT>(out, row, cols, padded, col, h);
   };

@@ -41,3 +41,17 @@ def test_gammas_that_bring_a_row_back(fmt):
     got = hago.mx_rmsnorm(x.to(t.DEV), gamma.to(t.DEV), eps=0.0, fmt=t.FORMATS[fmt])
     y = mx.rmsnorm(x.double().numpy(), gamma.double().numpy(), eps=0.0)[1]
     assert mx.accepts(t.host(got.codes), t.host(got.scales), y, t.NORM_DELTA, fmt)
+
+
+@pytest.mark.parametrize("cols", [1, 33, 300, 1100, 8200, 16400, 33000])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_a_row_that_is_no_number_leaves_the_room_behind_it_empty(cols, fmt):
+    """Blocks without a column keep zero codes and the scale byte 0, whatever the row holds (a NaN, or zeros without eps)."""
+    x = torch.randn(4, cols, generator=torch.Generator().manual_seed(2))
+    x[1, cols // 2], x[3] = float("nan"), 0.0
+    gamma = torch.ones(cols)
+    for g in (None, gamma):
+        got = hago.mx_rmsnorm(x.to(t.DEV), None if g is None else g.to(t.DEV), eps=0.0, fmt=t.FORMATS[fmt])
+        want = np.full((2, cols), np.nan)
+        codes, scales = mx.encode(want, fmt)
+        assert np.array_equal(t.host(got.scales)[[1, 3]], scales) and np.array_equal(t.host(got.codes)[[1, 3]], codes)
