@@ -201,12 +201,14 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const 
   } else {
     float h[8], g[8];
     double sum = 0;
-    for (int col = place * 8; col < padded; col += threads * 8) {
-      load(col, h);
+    const uint32_t end = padded;  // (a place behind the last one may lie beyond 2^31)
+    for (uint32_t at = place * 8; at < end; at += threads * 8) {
+      load((int)at, h);
       sum = square(h, sum);
     }
     const double factor = factor_of(sum);
-    for (int col = place * 8; col < padded; col += threads * 8) {
+    for (uint32_t at = place * 8; at < end; at += threads * 8) {
+      const int col = (int)at;
       load(col, h);
       if (gamma) mx_load8<TYPE>(gamma + col, cols - col, g);
       finish(col, h, factor, g);
