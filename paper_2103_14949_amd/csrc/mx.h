@@ -44,7 +44,7 @@ struct MxGemmArgs {
   const int32_t* index;    // or NULL
   int32_t T, N, K, a_rows, experts;
   int32_t type;            // of out
-  uint32_t grid;           // workgroups of the launch
+  uint32_t place;          // of the launch: its first tile, or how many workgroups there are where they stay for several tiles
 };
 // Most tiles of `rows` rows that the groups' rows can make: each has at least one row, each group at most one that is not full.
 constexpr int64_t mx_most_tiles(int64_t T, int64_t experts, int64_t rows) {

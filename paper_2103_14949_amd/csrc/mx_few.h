@@ -27,7 +27,8 @@ __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(HAGO_MX_GEMM
   const int lane = threadIdx.x & 63, part = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int tiles_p = (g.N + BP - 1) / BP;
-  const int tile_q = (int)(blockIdx.x / (uint32_t)tiles_p), p0 = (int)(blockIdx.x % (uint32_t)tiles_p) * BP;
+  const uint32_t tile = g.place + blockIdx.x;
+  const int tile_q = (int)(tile / (uint32_t)tiles_p), p0 = (int)(tile % (uint32_t)tiles_p) * BP;
   const MxGroups<BQ> groups(g);
   if (tile_q >= groups.tiles) return;
   const MxRows rows = groups.rows(g, tile_q);
@@ -131,7 +132,7 @@ hipError_t launch_few(const MxGemmArgs& g, int waves, hipStream_t st) {
   static_assert(kMostFewWaves * BP * BQ * sizeof(float) <= 65536, "LDS without a raised limit");
   const int64_t tiles_q = g.offsets ? mx_most_tiles(g.T, g.experts, BQ) : (g.T + BQ - 1) / BQ;
   const int64_t tiles = (int64_t)((g.N + BP - 1) / BP) * tiles_q;
-  return launch_mx_product(mx_few_kernel<FA, TP, TQ>, (unsigned)tiles, 64 * waves, waves * BP * BQ * sizeof(float), st, g);
+  return launch_mx_tiles(mx_few_kernel<FA, TP, TQ>, tiles, 64 * waves, waves * BP * BQ * sizeof(float), st, g);
 }
 
 }  // namespace

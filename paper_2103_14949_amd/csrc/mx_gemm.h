@@ -12,13 +12,23 @@ typedef float mx_v16f __attribute__((ext_vector_type(16)));
 
 // A kernel's arguments one by one: the first 14 dwords are in registers when a wavefront starts, where a struct would be fetched first.
 #define HAGO_MX_GEMM_PARAMETERS                                                                                                              \
-  const uint8_t *a, const uint8_t *w, const uint8_t *w_scale, const uint8_t *a_scale, int32_t T, int32_t N, int32_t K, uint32_t grid,      \
+  const uint8_t *a, const uint8_t *w, const uint8_t *w_scale, const uint8_t *a_scale, int32_t T, int32_t N, int32_t K, uint32_t place,     \
       const int32_t *offsets, const int32_t *index, const float *bias, void *out, int32_t a_rows, int32_t experts, int32_t type
-#define HAGO_MX_GEMM_STRUCT MxGemmArgs{a, a_scale, w, w_scale, bias, out, offsets, index, T, N, K, a_rows, experts, type, grid}
+#define HAGO_MX_GEMM_STRUCT MxGemmArgs{a, a_scale, w, w_scale, bias, out, offsets, index, T, N, K, a_rows, experts, type, place}
 template <typename Kernel>
-[[nodiscard]] inline hipError_t launch_mx_product(Kernel kern, unsigned grid, int threads, size_t lds, hipStream_t st, const MxGemmArgs& g) {
-  return launch_kernel(kern, dim3(grid), dim3(threads), lds, st, g.a, g.w, g.w_scale, g.a_scale, g.T, g.N, g.K, (uint32_t)grid, g.offsets, g.index, g.bias, g.out, g.a_rows,
+[[nodiscard]] inline hipError_t launch_mx_at(Kernel kern, int64_t grid, uint32_t place, int threads, size_t lds, hipStream_t st, const MxGemmArgs& g) {
+  return launch_kernel(kern, dim3((unsigned)grid), dim3(threads), lds, st, g.a, g.w, g.w_scale, g.a_scale, g.T, g.N, g.K, place, g.offsets, g.index, g.bias, g.out, g.a_rows,
                        g.experts, g.type);
+}
+// A workgroup per tile.  Many tiles go in several launches, each of whole eighths, so that a tile's XCD is the one it has among all.
+template <typename Kernel>
+[[nodiscard]] inline hipError_t launch_mx_tiles(Kernel kern, int64_t tiles, int threads, size_t lds, hipStream_t st, const MxGemmArgs& g) {
+  const int64_t most = max_blocks(threads) / 8 * 8;
+  for (int64_t first = 0; first < tiles; first += most) {
+    const hipError_t e = launch_mx_at(kern, tiles - first < most ? tiles - first : most, (uint32_t)first, threads, lds, st, g);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // cbsz / blgp of the scaled matrix instructions

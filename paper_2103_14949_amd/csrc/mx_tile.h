@@ -182,7 +182,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   const int tiles_p = (g.N + BP - 1) / BP;
   const MxGroups<BQ> groups(g);
   const uint32_t count = (uint32_t)tiles_p * (uint32_t)groups.tiles;
-  uint32_t id = blockIdx.x;
+  uint32_t id = Tile::STAYS ? blockIdx.x : g.place + blockIdx.x;
   if (id >= count) return;
   struct Place {
     MxRows rows;
@@ -371,10 +371,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   static_assert(SLOTS * ISSUES <= 63, "loads that can be counted");
   for (;;) {
     // the next tile's rows are looked up now and used when this one's loads have all gone out
-    more = Tile::STAYS && id + g.grid < count;
+    more = Tile::STAYS && id + g.place < count;
     Place next = here;
     Picked picked;
-    if (more) next = place_of(id + g.grid);
+    if (more) next = place_of(id + g.place);
     if (more) picked = pick_rows(next);
     auto bind_next = [&](int kt) {
       if (more && kt + SLOTS >= stages) bind(next, picked);
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
     // (every lane of a whole tile stores, so that the stores can be counted)
     stores = nq == BQ && n0 + TP * 32 <= g.N ? (g.type == kMxF32 ? kStores32 : kStores16) : 0;
     first = false;
-    id += g.grid;
+    id += g.place;
     here = next;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may be on its way into LDS that is given back)
@@ -465,7 +465,9 @@ hipError_t launch_tile(const MxGemmArgs& g, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int64_t tiles_q = g.offsets ? mx_most_tiles(g.T, g.experts, Tile::BQ) : (g.T + Tile::BQ - 1) / Tile::BQ;
   const int64_t tiles = (int64_t)((g.N + Tile::BP - 1) / Tile::BP) * tiles_q;
-  return launch_mx_product(kern, (unsigned)(Tile::STAYS && tiles > 256 * Tile::RESIDENT ? 256 * Tile::RESIDENT : tiles), Tile::NT, Tile::LDS, st, g);
+  const int64_t resident = tiles < 256 * Tile::RESIDENT ? tiles : 256 * Tile::RESIDENT;
+  if (Tile::STAYS) return launch_mx_at(kern, resident, (uint32_t)resident, Tile::NT, Tile::LDS, st, g);
+  return launch_mx_tiles(kern, tiles, Tile::NT, Tile::LDS, st, g);
 }
 
 }  // namespace

@@ -17,6 +17,7 @@ inline int calls = 0, refused = -1, launches_after = 0;
 inline hipError_t pending = hipSuccess;
 alignas(256) inline char scratch[256];
 inline std::string launched;   // the kernels launched, one a line
+inline void (*seen)(dim3 grid, dim3 block, void** args) = nullptr;   // called for each of them
 
 inline std::map<const void*, std::string>& names() {   // (filled while the library is loaded, before any constructor here)
   static std::map<const void*, std::string> all;
@@ -38,7 +39,10 @@ T* at(int n) { return reinterpret_cast<T*>((uintptr_t)(n + 1) << 28); }   // an 
 }  // namespace fake
 
 extern "C" {
-hipError_t hipLaunchKernel(const void* f, dim3, dim3, void**, size_t, hipStream_t) { return fake::answer(f); }
+hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, size_t, hipStream_t) {
+  if (fake::seen) fake::seen(grid, block, args);
+  return fake::answer(f);
+}
 hipError_t hipGetLastError() {
   const hipError_t e = fake::pending;
   fake::pending = hipSuccess;
