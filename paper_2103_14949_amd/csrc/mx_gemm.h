@@ -40,32 +40,34 @@ struct MxRows {
   int expert, row, end;
 };
 
-// One wavefront's look at 64 groups: lane l has group first + l.  The tiles of this and the groups before it are counted up.
+// One wavefront's look at 64 groups: lane l has group first + l.  The tiles of this and the groups before it are counted up, to
+// 2^32 - 1 at most: offsets that decrease can stand for more.
 struct MxScan {
-  int lo, hi, upto, here;
+  int lo, hi;
+  uint32_t upto, here;
 };
 template <int ROWS>
-__device__ __forceinline__ MxScan mx_scan(const int32_t* offsets, int T, int experts, int first, int before) {
+__device__ __forceinline__ MxScan mx_scan(const int32_t* offsets, int T, int experts, int first, uint32_t before) {
   const int lane = (int)threadIdx.x & 63, e = first + lane;
   MxScan s{0, 0, 0, 0};
   if (e < experts) {
     // (what lies outside the rows is none of theirs, whatever the array holds)
     s.lo = min(max(offsets[e], 0), T);
     s.hi = min(max(offsets[e + 1], s.lo), T);
-    s.here = (int)((uint32_t)(s.hi - s.lo + ROWS - 1) / ROWS);
+    s.here = (uint32_t)(s.hi - s.lo + ROWS - 1) / ROWS;
   }
   s.upto = s.here;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int o = __shfl_up(s.upto, d);
-    if (lane >= d) s.upto += o;
+    const uint32_t o = (uint32_t)__shfl_up((int)s.upto, d);
+    if (lane >= d) s.upto = __builtin_elementwise_add_sat(s.upto, o);
   }
-  s.upto += before;
+  s.upto = __builtin_elementwise_add_sat(s.upto, before);
   return s;
 }
 
-// The tiles of all groups, found by their numbers.  Up to 64 groups stay in registers, one a lane; of more the array is gone
-// through again for every tile.
+// The tiles of all groups, found by their numbers, and of those no more than the launch reckons with.  Up to 64 groups stay in registers, one a
+// lane; of more the array is gone through again for every tile.
 template <int ROWS>
 struct MxGroups {
   MxScan first;
@@ -77,22 +79,25 @@ struct MxGroups {
       return;
     }
     first = mx_scan<ROWS>(g.offsets, g.T, g.experts, 0, 0);
-    tiles = __builtin_amdgcn_readlane(first.upto, 63);
-    for (int e = 64; e < g.experts; e += 64) tiles = __builtin_amdgcn_readlane(mx_scan<ROWS>(g.offsets, g.T, g.experts, e, tiles).upto, 63);
+    uint32_t all = last(first);
+    for (int e = 64; e < g.experts; e += 64) all = last(mx_scan<ROWS>(g.offsets, g.T, g.experts, e, all));
+    tiles = (int)min(all, min((uint32_t)g.T / ROWS + (uint32_t)g.experts, (uint32_t)g.T));
   }
+  static __device__ __forceinline__ uint32_t last(const MxScan& s) { return (uint32_t)__builtin_amdgcn_readlane((int)s.upto, 63); }
   // tile: uniform, below `tiles`
   __device__ __forceinline__ MxRows rows(const MxGemmArgs& g, int tile) const {
     if (!g.offsets) return {0, tile * ROWS, g.T};
     MxScan s = first;
-    for (int e = 0;; e += 64) {
-      if (e) s = mx_scan<ROWS>(g.offsets, g.T, g.experts, e, __builtin_amdgcn_readlane(s.upto, 63));
-      const uint64_t there = __ballot(tile < s.upto);
+    for (int e = 0; e < g.experts; e += 64) {
+      if (e) s = mx_scan<ROWS>(g.offsets, g.T, g.experts, e, last(s));
+      const uint64_t there = __ballot((uint32_t)tile < s.upto);
       if (there) {
         const int l = __builtin_ctzll(there);
-        const int lo = __builtin_amdgcn_readlane(s.lo, l), upto = __builtin_amdgcn_readlane(s.upto, l), here = __builtin_amdgcn_readlane(s.here, l);
-        return {e + l, lo + (tile - (upto - here)) * ROWS, __builtin_amdgcn_readlane(s.hi, l)};
+        const int lo = __builtin_amdgcn_readlane(s.lo, l), before = __builtin_amdgcn_readlane((int)(s.upto - s.here), l);
+        return {e + l, lo + (tile - before) * ROWS, __builtin_amdgcn_readlane(s.hi, l)};
       }
     }
+    return {0, 0, 1};  // (only where the array changes under way: a row that is there)
   }
 };
 
