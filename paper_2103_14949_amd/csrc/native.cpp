@@ -617,25 +617,27 @@ PyObject* g_mx = nullptr;  // the binding's class MX(codes, scales, fmt, cols)
 // What such an operator returns: an MX, and behind it the residual and the values where they are asked for (a tuple then).
 // `out` is None or an MX whose tensors are taken; residual and values are True, a tensor, or False (values: or None).
 struct MxResults {
-  PyObject* all;
-  void *codes, *scales, *residual = nullptr, *values = nullptr;
+  PyObject* all = nullptr;
+  Ref code_tensor, scale_tensor;  // (the MX can be given others while a call is under way or prepared)
+  void *codes = nullptr, *scales = nullptr, *residual = nullptr, *values = nullptr;
+  MxResults(const at::Tensor& like, const MxRows& x, int64_t cols, PyObject* format, PyObject* out, PyObject* residual, PyObject* values);
 };
-MxResults mx_results(const at::Tensor& like, const MxRows& x, int64_t cols, PyObject* format, PyObject* out, PyObject* residual, PyObject* values) {
+MxResults::MxResults(const at::Tensor& like, const MxRows& x, int64_t cols, PyObject* format, PyObject* out, PyObject* keep_residual, PyObject* keep_values) {
   static PyObject *n_codes = intern("codes"), *n_scales = intern("scales"), *n_fmt = intern("fmt"), *n_cols = intern("cols");
   const int64_t f = as_int(format);
   require_format(f);
   const int64_t code_shape[2] = {x.rows, mx_code_bytes(cols, f)}, scale_shape[2] = {x.rows, mx_padded(cols) / 32}, shape[2] = {x.rows, cols};
-  const bool has_residual = residual != Py_False, has_values = values != Py_None && values != Py_False;
-  Ref mx, codes, scales, res, val;
+  const bool has_residual = keep_residual != Py_False, has_values = keep_values != Py_None && keep_values != Py_False;
+  Ref mx, res, val, &c = code_tensor, &s = scale_tensor;
   if (out != Py_None) {
     require(attr_int(out, n_fmt) == f && attr_int(out, n_cols) == cols);
-    codes.o = PyObject_GetAttr(out, n_codes);
-    scales.o = codes.o ? PyObject_GetAttr(out, n_scales) : nullptr;
-    if (!scales.o) throw Raised{};
-    tensor(codes.o), tensor(scales.o);
-    given(codes.o, at::IntArrayRef(code_shape, 2), at::kByte);
-    given(scales.o, at::IntArrayRef(scale_shape, 2), at::kByte);
-    on_current_device({codes.o, scales.o});
+    c.o = PyObject_GetAttr(out, n_codes);
+    s.o = c.o ? PyObject_GetAttr(out, n_scales) : nullptr;
+    if (!s.o) throw Raised{};
+    tensor(c.o), tensor(s.o);
+    given(c.o, at::IntArrayRef(code_shape, 2), at::kByte);
+    given(s.o, at::IntArrayRef(scale_shape, 2), at::kByte);
+    on_current_device({c.o, s.o});
     Py_INCREF(out);
     mx.o = out;
   }
@@ -644,35 +646,35 @@ MxResults mx_results(const at::Tensor& like, const MxRows& x, int64_t cols, PyOb
     if (o != Py_True) given(o, at::IntArrayRef(shape, 2), x.scalar), on_current_device({o});
     r.o = output(o == Py_True ? Py_None : o, at::IntArrayRef(shape, 2), x.scalar, like);
   };
-  optional(residual, has_residual, res);
-  optional(values, has_values, val);
+  optional(keep_residual, has_residual, res);
+  optional(keep_values, has_values, val);
   if (!mx.o) {
-    codes.o = output(Py_None, at::IntArrayRef(code_shape, 2), at::kByte, like);
-    scales.o = output(Py_None, at::IntArrayRef(scale_shape, 2), at::kByte, like);
-    Ref c;
-    c.o = PyLong_FromLongLong(cols);
-    PyObject* args[4] = {codes.o, scales.o, format, c.o};
-    mx.o = c.o ? PyObject_Vectorcall(g_mx, args, 4, nullptr) : nullptr;
+    c.o = output(Py_None, at::IntArrayRef(code_shape, 2), at::kByte, like);
+    s.o = output(Py_None, at::IntArrayRef(scale_shape, 2), at::kByte, like);
+    Ref n;
+    n.o = PyLong_FromLongLong(cols);
+    PyObject* args[4] = {c.o, s.o, format, n.o};
+    mx.o = n.o ? PyObject_Vectorcall(g_mx, args, 4, nullptr) : nullptr;
     if (!mx.o) throw Raised{};
   }
-  MxResults r{nullptr, tensor(codes.o).data_ptr(), tensor(scales.o).data_ptr(), has_residual ? tensor(res.o).data_ptr() : nullptr,
-              has_values ? tensor(val.o).data_ptr() : nullptr};
+  codes = tensor(c.o).data_ptr(), scales = tensor(s.o).data_ptr();
+  if (has_residual) residual = tensor(res.o).data_ptr();
+  if (has_values) values = tensor(val.o).data_ptr();
   auto take = [](Ref& v) {
     PyObject* o = v.o;
     v.o = nullptr;
     return o;
   };
   if (!has_residual && !has_values) {
-    r.all = take(mx);
-    return r;
+    all = take(mx);
+    return;
   }
-  r.all = PyTuple_New(1 + has_residual + has_values);
-  if (!r.all) throw Raised{};
+  all = PyTuple_New(1 + has_residual + has_values);
+  if (!all) throw Raised{};
   Py_ssize_t i = 0;
-  PyTuple_SET_ITEM(r.all, i++, take(mx));
-  if (has_residual) PyTuple_SET_ITEM(r.all, i++, take(res));
-  if (has_values) PyTuple_SET_ITEM(r.all, i++, take(val));
-  return r;
+  PyTuple_SET_ITEM(all, i++, take(mx));
+  if (has_residual) PyTuple_SET_ITEM(all, i++, take(res));
+  if (has_values) PyTuple_SET_ITEM(all, i++, take(val));
 }
 
 // mx_quantize, mx_silu_mul: (x, format, values, out, prepare)
@@ -685,8 +687,11 @@ PyObject* mx_quantize_with(Fn fn, bool gated, PyObject* const* a, Py_ssize_t n) 
   on_current_device({a[0]});
   const bool prepare = as_bool(a[4]);
   void* st = stream();
-  const MxResults r = mx_results(tensor(a[0]), x, cols, a[1], a[3], Py_False, a[2]);
-  return issue([=] { return fn(x.src, x.type, x.rows, cols, x.stride, (hago_mx_format)format, r.codes, r.scales, r.values, st); }, r.all, prepare, {a[0]});
+  const MxResults r(tensor(a[0]), x, cols, a[1], a[3], Py_False, a[2]);
+  return issue([=, codes = r.codes, scales = r.scales, values = r.values] {
+                 return fn(x.src, x.type, x.rows, cols, x.stride, (hago_mx_format)format, codes, scales, values, st);
+               },
+               r.all, prepare, {a[0], r.code_tensor.o, r.scale_tensor.o});
 }
 PyObject* f_mx_quantize(PyObject* const* a, Py_ssize_t n) { return mx_quantize_with(L.hago_mx_quantize, false, a, n); }
 PyObject* f_mx_silu_mul(PyObject* const* a, Py_ssize_t n) { return mx_quantize_with(L.hago_mx_silu_mul, true, a, n); }
@@ -706,10 +711,12 @@ PyObject* f_mx_rmsnorm(PyObject* const* a, Py_ssize_t n) {
   const bool prepare = as_bool(a[8]);
   PyObject* keep = a[7] != Py_None ? a[7] : a[2] != Py_None ? Py_True : Py_False;
   void* st = stream();
-  const MxResults r = mx_results(tensor(a[0]), x, x.columns, a[4], a[6], keep, a[5]);
-  return issue([=] { return L.hago_mx_rmsnorm(x.src, res, gamma, x.type, x.rows, x.columns, x.stride, (float)eps, (hago_mx_format)format, r.residual, r.codes,
-                                              r.scales, r.values, st); },
-               r.all, prepare, {a[0], a[1], a[2]});
+  const MxResults r(tensor(a[0]), x, x.columns, a[4], a[6], keep, a[5]);
+  return issue([=, residual = r.residual, codes = r.codes, scales = r.scales, values = r.values] {
+                 return L.hago_mx_rmsnorm(x.src, res, gamma, x.type, x.rows, x.columns, x.stride, (float)eps, (hago_mx_format)format, residual, codes, scales,
+                                          values, st);
+               },
+               r.all, prepare, {a[0], a[1], a[2], r.code_tensor.o, r.scale_tensor.o});
 }
 
 // An MX: its tensors (references of its own) and what they say.
