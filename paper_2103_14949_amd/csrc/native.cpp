@@ -107,12 +107,12 @@ at::ScalarType scalar_type(int64_t code) {
     case HAGO_I16: return at::kShort;
     case HAGO_I32: case HAGO_I24: return at::kInt;
     case HAGO_F32: return at::kFloat;
-    case HAGO_BF16: return at::kBFloat16;
-    case HAGO_F16: return at::kHalf;
   }
   PyErr_SetObject(PyExc_KeyError, PyLong_FromLongLong(code));
   throw Raised{};
 }
+// of the microscaled products' results
+at::ScalarType product_type(int64_t code) { return code == HAGO_BF16 ? at::kBFloat16 : code == HAGO_F16 ? at::kHalf : scalar_type(code); }
 
 // `given`, or a new tensor of the shape and type on `like`'s device (a new reference either way).
 PyObject* output(PyObject* given, at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
@@ -749,13 +749,13 @@ PyObject* f_mx_dense(PyObject* const* a, Py_ssize_t n) {
   require(w.format == HAGO_MX_FP4 && w.cols == act.cols);
   const int64_t M = act.rows, N = w.rows, K = act.cols, shape[2] = {M, N}, format = act.format, type = as_int(a[3]);
   given(a[2], at::IntArrayRef(&N, 1), at::kFloat);
-  given(a[4], at::IntArrayRef(shape, 2), scalar_type(type));
+  given(a[4], at::IntArrayRef(shape, 2), product_type(type));
   on_current_device({act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[4]});
   const float* bias = static_cast<const float*>(pointer(a[2]));
   const bool prepare = as_bool(a[5]);
   const void *ac = act.code_ptr(), *as = act.scale_ptr(), *wc = w.code_ptr(), *ws = w.scale_ptr();
   void* st = stream();
-  PyObject* out = output(a[4], at::IntArrayRef(shape, 2), scalar_type(type), tensor(act.codes.o));
+  PyObject* out = output(a[4], at::IntArrayRef(shape, 2), product_type(type), tensor(act.codes.o));
   void* dst = pointer(out);
   return issue([=] { return L.hago_mx_dense(ac, as, (hago_mx_format)format, wc, ws, bias, M, N, K, (hago_dtype)type, dst, st); }, out, prepare,
                {act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2]});
@@ -777,7 +777,7 @@ PyObject* f_mx_dense_grouped(PyObject* const* a, Py_ssize_t n) {
   }
   const int64_t shape[2] = {T, N};
   given(a[4], at::IntArrayRef(bias_shape, 2), at::kFloat);
-  given(a[6], at::IntArrayRef(shape, 2), scalar_type(type));
+  given(a[6], at::IntArrayRef(shape, 2), product_type(type));
   on_current_device({act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[3], a[4], a[6]});
   const int32_t *offsets = static_cast<const int32_t*>(pointer(a[2])), *index = static_cast<const int32_t*>(pointer(a[3]));
   const float* bias = static_cast<const float*>(pointer(a[4]));
@@ -785,7 +785,7 @@ PyObject* f_mx_dense_grouped(PyObject* const* a, Py_ssize_t n) {
   const void *ac = act.code_ptr(), *as = act.scale_ptr(), *wc = w.code_ptr(), *ws = w.scale_ptr();
   const int64_t a_rows = act.rows;
   void* st = stream();
-  PyObject* out = output(a[6], at::IntArrayRef(shape, 2), scalar_type(type), tensor(act.codes.o));
+  PyObject* out = output(a[6], at::IntArrayRef(shape, 2), product_type(type), tensor(act.codes.o));
   void* dst = pointer(out);
   return issue([=] { return L.hago_mx_dense_grouped(ac, as, (hago_mx_format)format, a_rows, index, wc, ws, bias, offsets, T, E, N, K, (hago_dtype)type, dst, st); },
                out, prepare, {act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[3], a[4]});
