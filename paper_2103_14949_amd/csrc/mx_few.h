@@ -19,7 +19,8 @@ namespace {
 
 constexpr int kMostFewWaves = 16;
 
-template <int FA, int TP, int TQ>
+// SPLIT: 8-bit rows in two parts (mx_split8), for 32-bit results.
+template <int FA, int TP, int TQ, bool SPLIT>
 __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(HAGO_MX_GEMM_PARAMETERS) {
   const MxGemmArgs g = HAGO_MX_GEMM_STRUCT;
   constexpr int BP = 16 * TP, BQ = 16 * TQ, PLANES = FA == kMxFp8 ? 2 : 1, STEPS = 4;
@@ -95,17 +96,23 @@ __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(HAGO_MX_GEMM
     for (int u = 0; u < STEPS; ++u) {
       if (step + u >= steps) break;
 #pragma unroll
-      for (int i = 0; i < TP; ++i)
+      for (int j = 0; j < TQ; ++j) {
+        const mx_v4i lo = af[u][j * PLANES], hi = af[u][j * PLANES + PLANES - 1];
+        mx_v8i q, low;
+        if constexpr (FA == kMxFp4) q = __builtin_shufflevector(lo, lo, 0, 1, 2, 3, -1, -1, -1, -1);
+        else q = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        if constexpr (SPLIT) mx_split8(q, q, low);
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) {
+        for (int i = 0; i < TP; ++i) {
           const mx_v8i p = __builtin_shufflevector(wf[u][i], wf[u][i], 0, 1, 2, 3, -1, -1, -1, -1);
-          const mx_v4i lo = af[u][j * PLANES], hi = af[u][j * PLANES + PLANES - 1];
-          mx_v8i q;
-          if constexpr (FA == kMxFp4) q = __builtin_shufflevector(lo, lo, 0, 1, 2, 3, -1, -1, -1, -1);
-          else q = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 0, (int)(wsf[i][u] >> shift), 0,
-                                                                       (int)(asf[j][u] >> shift));
+          const auto add = [&](const mx_v8i& part) {
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, part, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 0, (int)(wsf[i][u] >> shift), 0,
+                                                                         (int)(asf[j][u] >> shift));
+          };
+          add(q);
+          if constexpr (SPLIT) add(low);
         }
+      }
     }
   }
 
@@ -126,13 +133,13 @@ __global__ __launch_bounds__(64 * kMostFewWaves) void mx_few_kernel(HAGO_MX_GEMM
   }
 }
 
-template <int FA, int TP, int TQ>
+template <int FA, int TP, int TQ, bool SPLIT>
 hipError_t launch_few(const MxGemmArgs& g, int waves, hipStream_t st) {
   constexpr int BP = 16 * TP, BQ = 16 * TQ;
   static_assert(kMostFewWaves * BP * BQ * sizeof(float) <= 65536, "LDS without a raised limit");
   const int64_t tiles_q = g.offsets ? mx_most_tiles(g.T, g.experts, BQ) : (g.T + BQ - 1) / BQ;
   const int64_t tiles = (int64_t)((g.N + BP - 1) / BP) * tiles_q;
-  return launch_mx_tiles(mx_few_kernel<FA, TP, TQ>, tiles, 64 * waves, waves * BP * BQ * sizeof(float), st, g);
+  return launch_mx_tiles(mx_few_kernel<FA, TP, TQ, SPLIT>, tiles, 64 * waves, waves * BP * BQ * sizeof(float), st, g);
 }
 
 }  // namespace

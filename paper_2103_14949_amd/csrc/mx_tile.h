@@ -155,7 +155,8 @@ __device__ __forceinline__ void leave_by_quads(const MxGemmArgs& g, const mx_v16
     }
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB>
+// SPLIT: 8-bit rows in two parts (mx_split8), for 32-bit results.
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB, bool SPLIT>
 __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_PARAMETERS) {
   const MxGemmArgs g = HAGO_MX_GEMM_STRUCT;
   using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS, KB>;
@@ -308,6 +309,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   // the next 128 k's scales in front of them, and in the last group the loads of stage `dma_stage`.
   auto multiply = [&](mx_v16f (&acc)[TP][TQ], auto hconst, const uint8_t* next, int dma_stage, auto ring) {
     constexpr int H = decltype(hconst)::value, S = H & 1;
+    mx_v8i q_high, q_low;
     constexpr int reads = NR + (H % 2 ? TP + TQ : 0), each = (reads + NM - 1) / NM > 2 ? (reads + NM - 1) / NM : 2;
     [&]<int... Mi>(std::integer_sequence<int, Mi...>) {
       ([&] {
@@ -317,8 +319,16 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
         mx_v8i q;
         if constexpr (FA == kMxFp4) q = __builtin_shufflevector(q4, q4, 0, 1, 2, 3, -1, -1, -1, -1);
         else q = __builtin_shufflevector(q4, q5, 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 2 * (H % 2), (int)sc[i],
-                                                                    2 * (H % 2), (int)sc[TP + j]);
+        if constexpr (SPLIT) {
+          if constexpr (i == 0) mx_split8(q, q_high, q_low);
+          q = q_high;
+        }
+        const auto add = [&](const mx_v8i& part) {
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, part, acc[i][j], kMxMfmaFormat<kMxFp4>, kMxMfmaFormat<FA>, 2 * (H % 2), (int)sc[i],
+                                                                      2 * (H % 2), (int)sc[TP + j]);
+        };
+        add(q);
+        if constexpr (SPLIT) add(q_low);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = each * m; r < each * m + each && r < reads; ++r) {
@@ -360,7 +370,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   };
 
   auto by_type = [&](const auto& f) {
-    if (g.type == kMxF32) f.template operator()<kMxF32>();
+    if constexpr (SPLIT) f.template operator()<kMxF32>();
+    else if (FA == kMxFp4 && g.type == kMxF32) f.template operator()<kMxF32>();
     else if (g.type == kMxBf16) f.template operator()<kMxBf16>();
     else f.template operator()<kMxF16>();
   };
@@ -456,10 +467,10 @@ __global__ __launch_bounds__(64 * WP * WQ, 1) void mx_tile_kernel(HAGO_MX_GEMM_P
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may be on its way into LDS that is given back)
 }
 
-template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB>
+template <int FA, int WP, int WQ, int TP, int TQ, int SLOTS, int KB, bool SPLIT>
 hipError_t launch_tile(const MxGemmArgs& g, hipStream_t st) {
   using Tile = MxTile<FA, WP, WQ, TP, TQ, SLOTS, KB>;
-  const auto kern = mx_tile_kernel<FA, WP, WQ, TP, TQ, SLOTS, KB>;
+  const auto kern = mx_tile_kernel<FA, WP, WQ, TP, TQ, SLOTS, KB, SPLIT>;
   static std::atomic<uint64_t> attr_set{0};  // the devices whose dynamic-LDS limit is raised
   const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), Tile::LDS, attr_set);
   if (e != hipSuccess) return e;

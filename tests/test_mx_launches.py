@@ -26,7 +26,7 @@ def ask(tmp_path_factory):
 def shape(name):
     """Features, rows and threads of a kernel's tile, and whether its workgroups go from tile to tile."""
     kind, args = re.search(r"mx_(few|tile)_kernel<([^>]*)>", name).groups()
-    n = [int(v) for v in args.split(",")]
+    n = [int(v) for v in args.split(",") if v.strip() not in ("true", "false")]
     if kind == "few":
         return 16 * n[1], 16 * n[2], None, False
     _, wp, wq, tp, tq, slots, _ = n
