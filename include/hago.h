@@ -544,7 +544,8 @@ hago_status hago_probe_copy(const void* src, void* dst, int64_t bytes,
  * Test hook, not part of the operator set: forces which GEMM kernel family
  * and tile shape serve the following hago_qdense / hago_qconv2d* calls of
  * this process, so that tests can compare every variant with the oracle on
- * one shape.  Results never depend on it.  Keys:
+ * one shape.  Results never depend on it (but for the order in which the
+ * microscaled products add, each kernel's own).  Keys:
  *   HAGO_HOOK_GEMM_PATH     0 automatic; 1 the general register-staged kernel;
  *                           2 the streaming kernel, skipping the one-launch
  *                           convolution kernels; 3 the general one-launch

@@ -46,8 +46,8 @@ __device__ __forceinline__ void mx_load8(const typename MxElement<TYPE>::type* p
   }
 }
 
-// With the nontemporal hint: values and residuals are read much later than the codes beside them, if at all (norm of 8192 x 4096 bf16
-// with values 54 us without it, 49 so; codes alone of that size in 4 bits, with values, 33 and 23).
+// With the nontemporal hint: values and residuals are read much later than the codes beside them, if at all.  8192 x 4096 bf16 with
+// values, us without the hint and with it: the norm 55.5 and 50.6, the quantization to 4 bits 28.3 and 25.1.
 template <int TYPE>
 __device__ __forceinline__ void mx_store8(typename MxElement<TYPE>::type* p, int n, const float (&v)[8]) {
   using T = typename MxElement<TYPE>::type;

@@ -25,8 +25,9 @@ namespace {
 // About what a call takes in a kernel, in us.  A tile's time is `each` and `step` per stage of 256 k, workgroups of a round on a CU share it, and
 // alone it takes `alone` per stage, for it waits for its loads.  The constants are fitted to 3700 measured dense and grouped products of 1 to 16384
 // rows, 64 to 8192 features and k, weights from memory and not from the last-level cache, to the times and to the choice, longer calls counting more: what the
-// rule picks is 2.3 % slower than the fastest kernel on the average (2.4 % on the quarter of the products that was left out of the fit), 13 % in one
-// of twenty.  Examples, 8192 rows through 8192 x 8192: 4-bit rows 276 us with 256 x 256 tiles, 356 with 128 x 128, 502 with 128 x 64; 8-bit rows 390 with
+// rule picks is 2.3 % slower than the fastest kernel on the average, 13 % in one of twenty, 52 % at worst (figures of the products that the fit has
+// seen).  It reckons with rows that fall to groups by chance; where they do not, us of the pick and of the fastest: 8-bit rows through 4096 x 2048, 4096 rows,
+// half of them in one of 32 groups, 66 and 47, 16384 rows 153 and 143, 64 rows all in one of 64 groups 9.1 and 7.1.  Examples, 8192 rows through 8192 x 8192: 4-bit rows 276 us with 256 x 256 tiles, 356 with 128 x 128, 502 with 128 x 64; 8-bit rows 390 with
 // 256 x 256, 453 with 256 x 128, 618 with 128 x 64.  1024 rows through 4096 x 4096: 4-bit 28.3, 16.0, 17.4; 8-bit 37.9, 27.9, 22.1.
 // 300 rows there: 128 x 64 12.3 and 13.8, 64 x 64 10.3 and 12.5.
 struct MxShape {

@@ -2,8 +2,8 @@
 // addition), and behind a gated activation.
 //
 // A lane takes eight consecutive columns, a quad of lanes a block of 32: the block's largest magnitude takes two lane exchanges, and
-// the codes leave as 4 or 8 consecutive bytes per lane.  All three move bytes and little else: 8192 x 8192 fp32 to 4 bits with values in 100 us, norm
-// of 8192 x 4096 bf16 with residual and values in 51, activation of 16384 x 4096 bf16 with values in 84 (5.7, 5.9 and 5.6 TB/s; a copy of 1 GiB 5.0).
+// the codes leave as 4 or 8 consecutive bytes per lane.  All three move bytes and little else: 8192 x 8192 fp32 to 4 bits with values in 99 us, norm
+// of 8192 x 4096 bf16 with residual and values in 51, activation of 16384 x 4096 bf16 with values in 82 (5.8, 5.9 and 5.7 TB/s; a copy of 1 GiB by hago_probe_copy 6.3).
 #include "mx_device.h"
 
 namespace hago {
@@ -16,7 +16,8 @@ constexpr int kThreads = 256;
 
 // g / (1 + e^-g) * u within a few units of the last place.  e^-g is 2^t with t = -g log2 e in two parts, the quotient takes one correction.  From -80 on e^-g
 // stays below 2^116, so that its reciprocal is a normal number; above 80 the quotient is g.
-// (16384 x 4096 bf16 with values: 105 us with expf and the division, rounded once each, 100 so, 84 with one place per thread and hinted stores.)
+// (16384 x 4096 bf16 with values: 105 us with expf and the division, rounded once each, 100 with this quotient, 84 with one place per thread and
+// hinted stores, 82 since far gates are none of its business.)
 constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147182f, kFarGate = -80.0f;
 __device__ __forceinline__ float silu_mul(float g, float u) {
   const float t = g * -kLog2e;

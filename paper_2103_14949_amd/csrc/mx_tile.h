@@ -8,11 +8,11 @@
 //
 // What bounds it.  The matrix instructions alone run at 6800 (4-bit rows) and 4200 TFLOP/s (8-bit rows) on such codes; 8192 rows through
 // 8192 x 8192 take 265 us (4150) and 390 us (2820).  The matrix unit is busy for 56 % and 74 % of the cycles, at 1.6 GHz of 2.4: power sets the
-// clock, and the fragments' reads of LDS fill the rest.  So the tile is the one with the fewest bytes of LDS per instruction that the registers hold, 256 x 256 by
-// eight wavefronts of 128 x 64.  8-bit rows leave no room for two stages of 256 k of it (197 KB); three of 128 k fit (150 KB): 390 us, and 453 with
+// clock.  The tile is 256 x 256 by eight wavefronts of 128 x 64, 0.75 KB of LDS per instruction; four of 128 x 128, with
+// 0.5 KB, take 283 us against 260 with 4-bit rows, so those bytes are not all of the rest.  The 6.4 M cycles of bank conflicts counted with 4-bit rows are
+// the reads of scales, of which a stage of 256 k has 8 bytes a row (one of 128 k has 4, and none).  8-bit rows leave no room for two stages of 256 k of it (197 KB); three of 128 k fit (150 KB): 390 us, and 453 with
 // 256 x 128 tiles of two stages of 256 k.  4-bit rows with stages of 128 k in four slots take 331 us instead of 276, 128 x 128 tiles 512 instead of 356:
-// a row's half line is fetched twice and there are twice the barriers.  Other forms: four wavefronts of 128 x 128 with 4-bit rows 283 us against 260, a
-// higher priority for wavefronts in matrix instructions no difference.
+// a row's half line is fetched twice and there are twice the barriers.  A higher priority for wavefronts in matrix instructions made no difference.
 //
 // A workgroup stays for several tiles where the loads of the next one's first stages fit behind the last one's (Tile::STAYS).  Results leave
 // from the registers by pieces of whole 64 bytes that quads of lanes exchange, and by LDS where a wavefront has one 32-feature block only.
