@@ -26,7 +26,7 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
   const float d = 1.0f + __builtin_fmaf(e, rest * kLn2, e);
   const float r = __builtin_amdgcn_rcpf(d);
   const float q = g * r;
-  const float s = __builtin_fmaf(__builtin_fmaf(-q, d, g), r, q);
+  const float s = __builtin_fmaf(__builtin_fmaf(q, d, -g), -r, q);  // (in these signs -0 stays -0)
   return (g <= 80.0f ? s : g) * u;  // (the comparison fails for a NaN, which is g itself)
 }
 
@@ -149,9 +149,10 @@ __global__ __launch_bounds__(1024) void mx_rmsnorm_kernel(const void* x_, const 
       const float f = (float)factor, rest = (float)(factor - f);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float p = h[k] * f, e = __builtin_fmaf(h[k], rest, __builtin_fmaf(h[k], f, -p));
+        // (what is left of the products with its sign turned: so -0 stays -0)
+        const float p = h[k] * f, e = __builtin_fmaf(-h[k], rest, __builtin_fmaf(-h[k], f, p));
         const float y = p * g[k];
-        h[k] = gamma ? y + __builtin_fmaf(e, g[k], __builtin_fmaf(p, g[k], -y)) : p + e;
+        h[k] = gamma ? y - __builtin_fmaf(e, g[k], __builtin_fmaf(-p, g[k], y)) : p - e;
       }
     } else {  // (rows at the ends of binary32, where the factor or its second part is no normal number of it, and rows that have no factor)
 #pragma unroll
