@@ -507,6 +507,130 @@ hago_status hago_mx_dense_grouped(const void* a_codes, const void* a_scales,
                                   int64_t K, hago_dtype out_t, void* out,
                                   void* stream);
 
+/*
+ * Rotary positions.  x[T, heads, dim] -> out: the pairs j < `pairs` of every
+ * row's columns (a, b) = (j, j + pairs), or (2j, 2j + 1) for
+ * HAGO_ROPE_NEIGHBOURS, turned by t = positions[axis[j], row] * frequencies[j]:
+ *     out[a] = x[a] cos t - x[b] sin t      out[b] = x[b] cos t + x[a] sin t
+ * and the columns from 2 pairs on as they are.  positions [axes, T] (time,
+ * height, width or any others), frequencies [pairs], axis [pairs] (NULL: all 0)
+ * are device arrays; a pair whose axis is not below `axes` has position 0 (the
+ * caller's contract is that there is none).  The angle, its turns and their
+ * fraction are binary64, so positions may be far; cosines and sums are binary32,
+ * rounded once to x_t (HAGO_F32, HAGO_BF16 or HAGO_F16).
+ * Rows and heads of x and out may have any distance (in elements), so that the
+ * queries and keys of one product's result are turned by one call.  out may be x
+ * with the same strides, and not overlap it otherwise.
+ * Errors: NULL, SHAPE (negative; dim above 4096, heads above 65536, T beyond
+ * 2^31 - 1, 2 pairs above dim, axes < 1; strides negative, or such that rows or heads of
+ * out overlap), DTYPE, PARAM (order; misaligned for its elements; out is x with
+ * other strides), DEVICE.  Empty tensors are a no-op.
+ */
+typedef enum { HAGO_ROPE_HALVES = 0, HAGO_ROPE_NEIGHBOURS = 1 } hago_rope_order;
+hago_status hago_rope(const void* x, hago_dtype x_t, int64_t T, int64_t heads,
+                      int64_t dim, int64_t row_stride, int64_t head_stride,
+                      const int32_t* positions, int64_t axes,
+                      const float* frequencies, const int32_t* axis,
+                      int64_t pairs, hago_rope_order order, void* out,
+                      int64_t out_row_stride, int64_t out_head_stride,
+                      void* stream);
+
+/*
+ * A paged cache of keys and values on microscaled codes.  The codes of a token's
+ * key are those that hago_mx_quantize makes of it, in whole blocks of 32 columns
+ * (B = dim rounded up to 32, zero codes behind dim):
+ *   codes   [pages, kv_heads, page_size, B / 2 or B], 16-byte aligned
+ *   scales  [pages, kv_heads, page_size, B / 32]
+ * and the same for values; keys and values may differ in their format.  Codes of
+ * 8 bits that are no number (0x7f, 0xff), which the operators here never write,
+ * must not be in the pages of a sequence.
+ */
+typedef struct {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+  hago_mx_format k_format, v_format;
+  int64_t pages, kv_heads, page_size, dim;
+} hago_mx_cache;
+
+/*
+ * The sequences of a call, and which of its T rows are whose.  Position p of
+ * sequence s lies in page table[s * table_stride + p / page_size], at place
+ * p % page_size.  Its rows are offsets[s] .. offsets[s + 1] - 1, the last n of
+ * the lengths[s] tokens that it has with them: row i of n has position
+ * lengths[s] - n + i.  table [seqs, table_cols], lengths [seqs] and offsets
+ * [seqs + 1] are device arrays of int32; nothing waits for the device.
+ * A position below 0, at or behind table_cols * page_size, or whose entry is not
+ * below `pages` (a page that a window has left behind, say: -1) has no place: it is not
+ * written, not read, and no query sees it.  offsets do not decrease and lie in
+ * 0..T, and no two positions of a call share a place: the caller's contract, as
+ * device arrays' contents are (other values give wrong results, never an access
+ * out of bounds).  Rows in no sequence are left as they are.
+ */
+typedef struct {
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* offsets;
+  int64_t seqs, table_cols, table_stride;
+} hago_mx_sequences;
+
+/*
+ *   hago_mx_cache_write: the keys and values of T tokens, k and v [T, kv_heads,
+ *     dim] with rows and heads at any distance (in elements), into their places.
+ *     k_values and v_values, unless NULL, take the values that the codes stand
+ *     for, rounded to x_t once, as [T, kv_heads, dim] (also of tokens
+ *     without a place).
+ *   hago_mx_cache_read: the values of the rows' codes, rounded to out_t, into k
+ *     and v [T, kv_heads, dim]; rows without a place are left as they are.
+ * Real types are HAGO_F32, HAGO_BF16 and HAGO_F16.
+ * Errors: NULL (a pointer; the structs), SHAPE (negative; dim above 256,
+ * kv_heads above 65536, a cache of 2^62 bytes, pages, T or seqs beyond 2^31 - 1,
+ * page_size < 1, table_cols * page_size beyond 2^31 - 2^16, table_stride below
+ * table_cols; negative strides), DTYPE, PARAM (formats; misaligned), DEVICE.
+ * No tokens, sequences, heads or columns are a no-op.
+ */
+hago_status hago_mx_cache_write(const hago_mx_cache* cache,
+                                const hago_mx_sequences* sequences,
+                                const void* k, int64_t k_row_stride,
+                                int64_t k_head_stride, const void* v,
+                                int64_t v_row_stride, int64_t v_head_stride,
+                                hago_dtype x_t, int64_t T, void* k_values,
+                                void* v_values, void* stream);
+hago_status hago_mx_cache_read(const hago_mx_cache* cache,
+                               const hago_mx_sequences* sequences,
+                               hago_dtype out_t, int64_t T, void* k, void* v,
+                               void* stream);
+
+/*
+ * Attention of new tokens (one a sequence, a chunk, a prompt) over the cache that
+ * holds their keys and values already:
+ *     out[t, h] = sum_j e^(s_j) v_j / sum_j e^(s_j),   s_j = scale * q[t, h] k_j
+ * over the positions j of t's sequence that t sees: 0 <= j < lengths[s] that have
+ * a place, j <= p where `causal`, and j > p - window where window > 0 (p: t's own
+ * position).  Head h reads the cache's head h / (heads / kv_heads).  lse [T,
+ * heads], unless NULL, takes log(sum_j e^(s_j)).  A row that sees nothing gives
+ * zeros, and -infinity there.  q has rows and heads at any distance, out is dense.
+ * Codes and their scales go into the products as bfloat16, which holds them
+ * (below 2^-126 they may count as zero); queries and probabilities as one, two or
+ * three bfloat16 numbers for HAGO_BF16, HAGO_F16 and HAGO_F32; sums are binary32.
+ * workspace: device, 256-byte aligned, hago_mx_attention_workspace_bytes(...) bytes at
+ * least, of any contents; calls that may run at the same time need one each.
+ * Errors: as above, and SHAPE (heads not a multiple of kv_heads, T * heads beyond
+ * 2^27, seqs * kv_heads beyond 2^22; window negative), PARAM (scale
+ * not finite; workspace too small or misaligned).
+ * hago_mx_attention_workspace_bytes returns -1 for what the call would refuse.
+ */
+int64_t hago_mx_attention_workspace_bytes(int64_t T, int64_t heads,
+                                          int64_t kv_heads, int64_t dim);
+hago_status hago_mx_attention(const hago_mx_cache* cache,
+                              const hago_mx_sequences* sequences, const void* q,
+                              hago_dtype q_t, int64_t T, int64_t heads,
+                              int64_t q_row_stride, int64_t q_head_stride,
+                              float scale, int32_t causal, int64_t window,
+                              void* out, float* lse, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* hago_status_string(hago_status s);
 

@@ -12,6 +12,7 @@ from .binding import (  # noqa: F401
     U8, I8, I16, I32, F32, I24, NCHW, NHWC, STRICT_ACC16, WS_WEIGHTS_READY, STATIC_SCRATCH_BYTES, ROUND_UPWARD, ROUND_HALF_AWAY,
     HOOK_GEMM_PATH, HOOK_STREAM_TILE, HOOK_GENERAL_TILE, HOOK_MX_KERNEL,
     MX, MX_FP4, MX_FP8, BF16, F16, mx_quantize, mx_rmsnorm, mx_silu_mul, mx_dense, mx_dense_grouped,
+    rope, MXCache, mx_cache_write, mx_cache_read, mx_attention, mx_attention_workspace_bytes,
 )
 
 

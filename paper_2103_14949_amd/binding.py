@@ -27,6 +27,7 @@ _NATIVE_PATH = os.path.join(_HERE, "_native.so")
 
 EXPORTS = ("hago_simquant", "hago_simquant_batched", "hago_absmax", "hago_simquant_wrap", "hago_quantize", "hago_dequantize", "hago_simquant_codes", "hago_qdense", "hago_qconv2d", "hago_qconv2d_ws", "hago_qconv2d_workspace_bytes", "hago_qconv2d_static", "hago_requantize",
            "hago_mx_quantize", "hago_mx_rmsnorm", "hago_mx_silu_mul", "hago_mx_dense", "hago_mx_dense_grouped",
+           "hago_rope", "hago_mx_cache_write", "hago_mx_cache_read", "hago_mx_attention", "hago_mx_attention_workspace_bytes",
            "hago_status_string", "hago_bit_range", "hago_set_test_hook", "hago_probe_mfma_i8", "hago_probe_copy")
 
 
@@ -38,6 +39,17 @@ class _QType(C.Structure):
 class _Requant(C.Structure):
     _fields_ = [("multiplier", C.c_void_p), ("shift", C.c_void_p), ("per_channel", C.c_int32),
                 ("out", _QType), ("clip_lo", C.c_int32), ("clip_hi", C.c_int32), ("rounding", C.c_int32)]
+
+
+class _MxCache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+                ("k_format", C.c_int32), ("v_format", C.c_int32),
+                ("pages", C.c_int64), ("kv_heads", C.c_int64), ("page_size", C.c_int64), ("dim", C.c_int64)]
+
+
+class _MxSequences(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lengths", C.c_void_p), ("offsets", C.c_void_p),
+                ("seqs", C.c_int64), ("table_cols", C.c_int64), ("table_stride", C.c_int64)]
 
 
 class HagoError(RuntimeError):
@@ -107,6 +119,17 @@ def lib():
         L.hago_mx_dense.argtypes = [vp, vp, i32, vp, vp, vp, i64, i64, i64, i32, vp, vp]
         L.hago_mx_dense_grouped.restype = i32
         L.hago_mx_dense_grouped.argtypes = [vp, vp, i32, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, vp]
+        cache, seqs = C.POINTER(_MxCache), C.POINTER(_MxSequences)
+        L.hago_rope.restype = i32
+        L.hago_rope.argtypes = [vp, i32, i64, i64, i64, i64, i64, vp, i64, vp, vp, i64, i32, vp, i64, i64, vp]
+        L.hago_mx_cache_write.restype = i32
+        L.hago_mx_cache_write.argtypes = [cache, seqs, vp, i64, i64, vp, i64, i64, i32, i64, vp, vp, vp]
+        L.hago_mx_cache_read.restype = i32
+        L.hago_mx_cache_read.argtypes = [cache, seqs, i32, i64, vp, vp, vp]
+        L.hago_mx_attention_workspace_bytes.restype = i64
+        L.hago_mx_attention_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.hago_mx_attention.restype = i32
+        L.hago_mx_attention.argtypes = [cache, seqs, vp, i32, i64, i64, i64, i64, C.c_float, i32, i64, vp, vp, vp, i64, vp]
         L.hago_bit_range.restype = i32
         L.hago_bit_range.argtypes = [i32, i32, C.POINTER(i32), C.POINTER(i32)]
         L.hago_probe_mfma_i8.restype = i32
@@ -353,3 +376,60 @@ def mx_dense_grouped(a: MX, w: MX, offsets, rows=None, bias=None, out_dtype=BF16
     Result row t belongs to the group e with offsets[e] <= t < offsets[e + 1] and is made of a's row rows[t] (int32
     device tensor; None: row t); bias [E,N] float32.  Returns [T,N]; rows in no group are not written."""
     return (_native or _native_module()).mx_dense_grouped(a, w, offsets, rows, bias, out_dtype, out, prepare)
+
+
+def rope(x, positions, frequencies, axes=None, interleaved=False, out=None, prepare=False):
+    """hago_rope over x[T, heads, dim] (float32, bfloat16 or float16; rows and heads at any distance): a tensor like x.
+
+    positions [axes, T] (or [T]) int32 and frequencies [pairs] float32, on the device; axes [pairs] int32 says whose position turns a pair
+    (None: the first).  Pairs are columns j and j + pairs, interleaved 2j and 2j + 1.  out may be x itself, or any tensor of its shape that
+    does not overlap it."""
+    return (_native or _native_module()).rope(x, positions, frequencies, axes, interleaved, out, prepare)
+
+
+class MXCache:
+    """A paged cache of keys and values on microscaled codes (uint8 device tensors, laid out as include/hago.h says): codes
+    [pages, kv_heads, page_size, bytes], scales [pages, kv_heads, page_size, blocks], their formats and the columns of a row."""
+
+    __slots__ = ("k_codes", "k_scales", "v_codes", "v_scales", "k_fmt", "v_fmt", "dim")
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, k_fmt, v_fmt, dim):
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.k_fmt, self.v_fmt, self.dim = k_fmt, v_fmt, dim
+
+    @staticmethod
+    def empty(pages, kv_heads, page_size, dim, k_fmt=MX_FP8, v_fmt=None, device="cuda"):
+        """Room for `pages` pages; v_fmt None: k_fmt."""
+        import torch
+        v_fmt, blocks = k_fmt if v_fmt is None else v_fmt, (dim + 31) // 32
+        room = lambda n: torch.empty(pages, kv_heads, page_size, n, dtype=torch.uint8, device=device)  # noqa: E731
+        wide = lambda fmt: blocks * (16 if fmt == MX_FP4 else 32)  # noqa: E731
+        return MXCache(room(wide(k_fmt)), room(blocks), room(wide(v_fmt)), room(blocks), k_fmt, v_fmt, dim)
+
+
+# The three operators of a cache take the sequences of a call as int32 device tensors: table [seqs, entries] (rows at any distance), lengths
+# [seqs] with the call's tokens, offsets [seqs + 1] of the rows.  Row i of a sequence's n has position lengths[s] - n + i.
+
+def mx_cache_write(cache: MXCache, k, v, table, lengths, offsets, values=False, prepare=False):
+    """hago_mx_cache_write of k, v [T, kv_heads, dim] (rows and heads at any distance): the cache.
+
+    values=True: the values that the codes stand for instead, as two tensors [T, kv_heads, dim]; rows in no sequence are not written."""
+    return (_native or _native_module()).mx_cache_write(cache, k, v, table, lengths, offsets, values, prepare)
+
+
+def mx_cache_read(cache: MXCache, table, lengths, offsets, rows, out_dtype=BF16, out=None, prepare=False):
+    """hago_mx_cache_read of `rows` rows: two tensors [rows, kv_heads, dim] of out_dtype (BF16, F16, F32); out: the two to take them."""
+    return (_native or _native_module()).mx_cache_read(cache, table, lengths, offsets, rows, out_dtype, out, prepare)
+
+
+def mx_attention_workspace_bytes(T, heads, kv_heads, dim):
+    """hago_mx_attention_workspace_bytes."""
+    return int(lib().hago_mx_attention_workspace_bytes(int(T), int(heads), int(kv_heads), int(dim)))
+
+
+def mx_attention(q, cache: MXCache, table, lengths, offsets, scale=None, causal=True, window=0, lse=False, out=None, workspace=None, prepare=False):
+    """hago_mx_attention of q [T, heads, dim] (rows and heads at any distance): a dense tensor like q.
+
+    scale None: dim ** -0.5; window 0: none.  lse=True, or a float32 tensor [T, heads]: (out, the logarithms of the sums).  Rows in no sequence are
+    not written.  workspace: a uint8 device tensor of mx_attention_workspace_bytes(...) bytes (None: a new one, which a prepared call keeps)."""
+    return (_native or _native_module()).mx_attention(q, cache, table, lengths, offsets, scale, causal, window, lse, out, workspace, prepare)

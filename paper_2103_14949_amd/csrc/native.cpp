@@ -13,6 +13,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <functional>
 #include <vector>
 
@@ -25,7 +26,8 @@ namespace {
   X(hago_simquant) X(hago_simquant_wrap) X(hago_simquant_batched) X(hago_quantize) X(hago_dequantize)              \
   X(hago_simquant_codes) X(hago_absmax) X(hago_requantize) X(hago_qdense) X(hago_qconv2d) X(hago_qconv2d_ws)       \
   X(hago_qconv2d_static) X(hago_bit_range) X(hago_mx_quantize) X(hago_mx_rmsnorm) X(hago_mx_silu_mul)                 \
-  X(hago_mx_dense) X(hago_mx_dense_grouped)
+  X(hago_mx_dense) X(hago_mx_dense_grouped) X(hago_rope) X(hago_mx_cache_write) X(hago_mx_cache_read)                 \
+  X(hago_mx_attention) X(hago_mx_attention_workspace_bytes)
 struct Library {
 #define X(name) decltype(&::name) name;
   HAGO_ENTRIES(X)
@@ -791,6 +793,196 @@ PyObject* f_mx_dense_grouped(PyObject* const* a, Py_ssize_t n) {
                out, prepare, {act.codes.o, act.scales.o, w.codes.o, w.scales.o, a[2], a[3], a[4]});
 }
 
+// ---- rotary positions, and the operators around a paged cache
+struct Heads {  // x[T, heads, dim], rows and heads at any distance
+  hago_dtype type;
+  at::ScalarType scalar;
+  int64_t T, heads, dim, row, head;
+  const void* src;
+};
+Heads heads_of(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  require(t.dim() == 3);
+  const int64_t T = t.size(0), heads = t.size(1), dim = t.size(2);
+  const bool any = t.numel() != 0;
+  require(!any || dim <= 1 || t.stride(2) == 1);
+  return {real_type(t), t.scalar_type(), T, heads, dim, any && T > 1 ? t.stride(0) : heads * dim, any && heads > 1 ? t.stride(1) : dim, t.data_ptr()};
+}
+
+// (x, positions, frequencies, axes, interleaved, out, prepare)
+PyObject* f_rope(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 7);
+  const Heads x = heads_of(a[0]);
+  const at::Tensor &positions = tensor(a[1]), &frequencies = tensor(a[2]);
+  const int64_t pairs = frequencies.numel(), axes = positions.dim() == 2 ? positions.size(0) : 1;
+  require(positions.scalar_type() == at::kInt && positions.is_contiguous() && (positions.dim() == 1 || positions.dim() == 2) &&
+          positions.size(positions.dim() - 1) == x.T && axes >= 1);
+  given(a[2], at::IntArrayRef(&pairs, 1), at::kFloat);
+  given(a[3], at::IntArrayRef(&pairs, 1), at::kInt);
+  require(2 * pairs <= x.dim);
+  const bool neighbours = as_bool(a[4]), prepare = as_bool(a[6]);
+  on_current_device({a[0], a[1], a[2], a[3], a[5]});
+  if (a[5] != Py_None) {
+    const Heads o = heads_of(a[5]);
+    require(o.scalar == x.scalar && o.T == x.T && o.heads == x.heads && o.dim == x.dim);
+  }
+  const int32_t *pos = positions.data_ptr<int32_t>(), *axis = static_cast<const int32_t*>(pointer(a[3]));
+  const float* freq = frequencies.data_ptr<float>();
+  void* st = stream();
+  const int64_t shape[3] = {x.T, x.heads, x.dim};
+  PyObject* out = output(a[5], at::IntArrayRef(shape, 3), x.scalar, tensor(a[0]));
+  const Heads y = heads_of(out);
+  void* dst = const_cast<void*>(y.src);
+  return issue([=] {
+                 return L.hago_rope(x.src, x.type, x.T, x.heads, x.dim, x.row, x.head, pos, axes, freq, axis, pairs, neighbours ? HAGO_ROPE_NEIGHBOURS : HAGO_ROPE_HALVES,
+                                    dst, y.row, y.head, st);
+               },
+               out, prepare, {a[0], a[1], a[2], a[3]});
+}
+
+// An MXCache and the sequences of a call.
+struct MxCacheOperand {
+  Ref t[4];  // codes and scales of keys, of values
+  hago_mx_cache cache;
+  hago_mx_sequences sequences;
+  PyObject *table, *lengths, *offsets;
+  MxCacheOperand(PyObject* o, PyObject* table, PyObject* lengths, PyObject* offsets) : table(table), lengths(lengths), offsets(offsets) {
+    static PyObject* const names[4] = {intern("k_codes"), intern("k_scales"), intern("v_codes"), intern("v_scales")};
+    static PyObject *k_fmt = intern("k_fmt"), *v_fmt = intern("v_fmt"), *n_dim = intern("dim");
+    const int64_t formats[2] = {attr_int(o, k_fmt), attr_int(o, v_fmt)}, dim = attr_int(o, n_dim), blocks = (dim + 31) / 32;
+    require_format(formats[0]), require_format(formats[1]);
+    require(dim >= 0);
+    for (int i = 0; i < 4; ++i) {
+      t[i].o = PyObject_GetAttr(o, names[i]);
+      if (!t[i].o) throw Raised{};
+      const at::Tensor& x = tensor(t[i].o);
+      require(x.dim() == 4 && x.scalar_type() == at::kByte && x.is_contiguous());
+      require(x.sizes().slice(0, 3) == tensor(t[0].o).sizes().slice(0, 3));
+      require(x.size(3) == (i % 2 ? blocks : blocks * (formats[i / 2] == HAGO_MX_FP4 ? 16 : 32)));
+    }
+    const at::Tensor &x = tensor(t[0].o), &b = tensor(table);
+    cache = {x.data_ptr(), tensor(t[1].o).data_ptr(), tensor(t[2].o).data_ptr(), tensor(t[3].o).data_ptr(), (hago_mx_format)formats[0], (hago_mx_format)formats[1],
+             x.size(0), x.size(1), x.size(2), dim};
+    require(b.dim() == 2 && b.scalar_type() == at::kInt);
+    const int64_t seqs = b.size(0), cols = b.size(1), ends = seqs + 1;
+    require(b.numel() == 0 || ((cols <= 1 || b.stride(1) == 1) && (seqs <= 1 || b.stride(0) >= cols)));
+    tensor(lengths), tensor(offsets);
+    given(lengths, at::IntArrayRef(&seqs, 1), at::kInt);
+    given(offsets, at::IntArrayRef(&ends, 1), at::kInt);
+    sequences = {static_cast<const int32_t*>(b.data_ptr()), tensor(lengths).data_ptr<int32_t>(), tensor(offsets).data_ptr<int32_t>(), seqs, cols,
+                 seqs > 1 && cols ? b.stride(0) : cols};
+  }
+  void on_device(std::initializer_list<PyObject*> others) const {
+    on_current_device({t[0].o, t[1].o, t[2].o, t[3].o, table, lengths, offsets});
+    on_current_device(others);
+  }
+};
+// A new reference to (a, b), whose references it takes over.
+PyObject* pair_of(Ref& a, Ref& b) {
+  PyObject* both = PyTuple_New(2);
+  if (!both) throw Raised{};
+  PyTuple_SET_ITEM(both, 0, a.o);
+  PyTuple_SET_ITEM(both, 1, b.o);
+  a.o = b.o = nullptr;
+  return both;
+}
+
+// (cache, k, v, table, lengths, offsets, values, prepare)
+PyObject* f_mx_cache_write(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 8);
+  const MxCacheOperand m(a[0], a[3], a[4], a[5]);
+  const Heads k = heads_of(a[1]), v = heads_of(a[2]);
+  require(k.scalar == v.scalar && k.T == v.T && k.heads == m.cache.kv_heads && v.heads == k.heads && k.dim == m.cache.dim && v.dim == k.dim);
+  m.on_device({a[1], a[2]});
+  const bool values = as_bool(a[6]), prepare = as_bool(a[7]);
+  void *st = stream(), *k_values = nullptr, *v_values = nullptr;
+  PyObject* out = a[0];
+  if (values) {
+    const int64_t shape[3] = {k.T, k.heads, k.dim};
+    Ref kv, vv;
+    kv.o = output(Py_None, at::IntArrayRef(shape, 3), k.scalar, tensor(a[1]));
+    vv.o = output(Py_None, at::IntArrayRef(shape, 3), k.scalar, tensor(a[1]));
+    k_values = pointer(kv.o), v_values = pointer(vv.o);
+    out = pair_of(kv, vv);
+  } else {
+    Py_INCREF(out);
+  }
+  return issue([=, cache = m.cache, sequences = m.sequences] {
+                 return L.hago_mx_cache_write(&cache, &sequences, k.src, k.row, k.head, v.src, v.row, v.head, k.type, k.T, k_values, v_values, st);
+               },
+               out, prepare, {m.t[0].o, m.t[1].o, m.t[2].o, m.t[3].o, a[1], a[2], a[3], a[4], a[5]});
+}
+
+// (cache, table, lengths, offsets, rows, out_dtype, out, prepare)
+PyObject* f_mx_cache_read(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 8);
+  const MxCacheOperand m(a[0], a[1], a[2], a[3]);
+  const int64_t T = as_int(a[4]), type = as_int(a[5]), shape[3] = {T, m.cache.kv_heads, m.cache.dim};
+  const at::ScalarType scalar = product_type(type);
+  require(T >= 0);
+  const bool prepare = as_bool(a[7]);
+  PyObject *kg = Py_None, *vg = Py_None;
+  if (a[6] != Py_None) {
+    require(PyTuple_Check(a[6]) && PyTuple_GET_SIZE(a[6]) == 2);
+    kg = PyTuple_GET_ITEM(a[6], 0), vg = PyTuple_GET_ITEM(a[6], 1);
+    tensor(kg), tensor(vg);
+    given(kg, at::IntArrayRef(shape, 3), scalar);
+    given(vg, at::IntArrayRef(shape, 3), scalar);
+  }
+  m.on_device({kg, vg});
+  void* st = stream();
+  Ref k, v;
+  k.o = output(kg, at::IntArrayRef(shape, 3), scalar, tensor(m.t[0].o));
+  v.o = output(vg, at::IntArrayRef(shape, 3), scalar, tensor(m.t[0].o));
+  void *kp = pointer(k.o), *vp = pointer(v.o);
+  return issue([=, cache = m.cache, sequences = m.sequences] { return L.hago_mx_cache_read(&cache, &sequences, (hago_dtype)type, T, kp, vp, st); }, pair_of(k, v),
+               prepare, {m.t[0].o, m.t[1].o, m.t[2].o, m.t[3].o, a[1], a[2], a[3]});
+}
+
+// (q, cache, table, lengths, offsets, scale, causal, window, lse, out, workspace, prepare)
+PyObject* f_mx_attention(PyObject* const* a, Py_ssize_t n) {
+  need_args(n, 12);
+  const MxCacheOperand m(a[1], a[2], a[3], a[4]);
+  const Heads q = heads_of(a[0]);
+  require(q.dim == m.cache.dim && (m.cache.kv_heads ? q.heads % m.cache.kv_heads == 0 : q.heads == 0));
+  double scale = q.dim ? 1.0 / std::sqrt((double)q.dim) : 1.0;
+  if (a[5] != Py_None) {
+    scale = PyFloat_AsDouble(a[5]);
+    if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
+  }
+  const bool causal = as_bool(a[6]), prepare = as_bool(a[11]);
+  const int64_t window = as_int(a[7]), shape[3] = {q.T, q.heads, q.dim};
+  const bool has_lse = a[8] != Py_None && a[8] != Py_False;
+  if (has_lse && a[8] != Py_True) tensor(a[8]), given(a[8], at::IntArrayRef(shape, 2), at::kFloat), on_current_device({a[8]});
+  given(a[9], at::IntArrayRef(shape, 3), q.scalar);
+  m.on_device({a[0], a[9], a[10]});
+  int64_t bytes = L.hago_mx_attention_workspace_bytes(q.T, q.heads, m.cache.kv_heads, q.dim);
+  if (a[10] != Py_None) {
+    const at::Tensor& w = tensor(a[10]);
+    require(w.scalar_type() == at::kByte && w.is_contiguous() && w.numel() >= bytes);
+  }
+  void* st = stream();
+  Ref out, lse, workspace;
+  out.o = output(a[9], at::IntArrayRef(shape, 3), q.scalar, tensor(a[0]));
+  if (has_lse) lse.o = output(a[8] == Py_True ? Py_None : a[8], at::IntArrayRef(shape, 2), at::kFloat, tensor(a[0]));
+  const int64_t room = bytes < 0 ? 0 : bytes;  // (the call says what is wrong)
+  workspace.o = output(a[10], at::IntArrayRef(&room, 1), at::kByte, tensor(a[0]));
+  void *dst = pointer(out.o), *w = pointer(workspace.o);
+  float* sums = has_lse ? static_cast<float*>(pointer(lse.o)) : nullptr;
+  bytes = tensor(workspace.o).numel();
+  PyObject* all;
+  if (has_lse) {
+    all = pair_of(out, lse);
+  } else {
+    all = out.o;
+    out.o = nullptr;
+  }
+  return issue([=, cache = m.cache, sequences = m.sequences] {
+                 return L.hago_mx_attention(&cache, &sequences, q.src, q.type, q.T, q.heads, q.row, q.head, (float)scale, causal, window, dst, sums, w, bytes, st);
+               },
+               all, prepare, {m.t[0].o, m.t[1].o, m.t[2].o, m.t[3].o, a[0], a[2], a[3], a[4], workspace.o});
+}
+
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -846,7 +1038,8 @@ PyMethodDef methods[] = {HAGO_METHOD(bind), HAGO_METHOD(entries), HAGO_METHOD(si
                          HAGO_METHOD(simquant_batched), HAGO_METHOD(quantize), HAGO_METHOD(simquant_codes),
                          HAGO_METHOD(dequantize), HAGO_METHOD(absmax), HAGO_METHOD(requantize), HAGO_METHOD(qdense),
                          HAGO_METHOD(qconv2d), HAGO_METHOD(mx_quantize), HAGO_METHOD(mx_silu_mul), HAGO_METHOD(mx_rmsnorm),
-                         HAGO_METHOD(mx_dense), HAGO_METHOD(mx_dense_grouped), {}};
+                         HAGO_METHOD(mx_dense), HAGO_METHOD(mx_dense_grouped), HAGO_METHOD(rope),
+                         HAGO_METHOD(mx_cache_write), HAGO_METHOD(mx_cache_read), HAGO_METHOD(mx_attention), {}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native marshalling of the libhago binding.", -1, methods};
 
 }  // namespace

@@ -1,0 +1,267 @@
+"""Attention over a paged microscaled cache on the GPU against the oracle in 64 bits, which works on the values that the codes stand for; see
+cache_util.attention_bound for how far a result may be off."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2103_14949_amd as hago
+from cache_util import DEV, FORMATS, TYPES, check_attention, layout, on_gpu, random_cache
+from oracle import cache_ref as ref
+
+
+def run(new, lengths, heads, kv_heads, dim, page, k_fmt="fp8", v_fmt="fp8", name="bf16", causal=True, window=0, scale=None, seed=0, rows_before=1, rows_behind=2):
+    rng = np.random.default_rng(seed)
+    table, lengths, offsets, pages = layout(new, lengths, page, seed=seed, rows_before=rows_before)
+    cache, keys, values = random_cache(rng, pages, kv_heads, page, dim, k_fmt, v_fmt)
+    T = int(offsets[-1]) + rows_behind
+    q = torch.from_numpy(rng.standard_normal((T, heads, dim))).to(TYPES[name])
+    out = torch.full((T, heads, dim), 7.0, dtype=TYPES[name], device=DEV)
+    lse = torch.full((T, heads), 7.0, device=DEV)
+    got = hago.mx_attention(q.to(DEV), cache, *on_gpu(table, lengths, offsets), scale=scale, causal=causal, window=window, lse=lse, out=out)
+    assert got[0] is out and got[1] is lse
+    _, inside = check_attention(out, name, q.double().numpy(), keys, values, ref.Sequences(table, lengths, offsets, pages, page), dim ** -0.5 if scale is None else scale,
+                                causal, window, lse)
+    assert (out.cpu()[torch.from_numpy(~inside)] == 7).all() and (lse.cpu()[torch.from_numpy(~inside)] == 7).all()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("k_fmt,v_fmt", [("fp8", "fp8"), ("fp8", "fp4"), ("fp4", "fp8"), ("fp4", "fp4")])
+@pytest.mark.parametrize("dim", [1, 32, 40, 64, 80, 96, 128, 160, 256])
+def test_formats_and_columns(dim, k_fmt, v_fmt, name):
+    run([1, 3], [70, 33], 4, 2, dim, 16, k_fmt, v_fmt, name, seed=dim)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 3), (8, 1), (15, 5), (16, 1), (17, 1), (40, 2)])
+@pytest.mark.parametrize("new,lengths", [([1], [1]), ([1], [129]), ([5, 0, 1, 2], [5, 7, 400, 31]), ([40], [40])])
+def test_heads_and_chunks(new, lengths, heads, kv_heads):
+    run(new, lengths, heads, kv_heads, 64, 32, seed=heads)
+
+
+@pytest.mark.parametrize("page", [1, 3, 16, 48, 64, 100, 1000])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 1), (True, 50), (False, 0), (False, 20), (True, 10 ** 6)])
+def test_pages_and_windows(page, causal, window):
+    run([9, 1, 30], [150, 77, 30], 4, 2, 64, page, "fp8", "fp4", causal=causal, window=window, seed=page)
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [15, 16, 17, 31, 32, 33, 127, 128, 129, 255, 257, 640, 2049])
+def test_lengths(length, name):
+    run([1, 2], [length, 2], 4, 1, 128, 64, name=name, seed=length)
+
+
+@pytest.mark.parametrize("window", [0, 3])
+def test_rows_that_see_nothing(window):
+    """More new tokens than the sequence has, lengths of zero and below: zeros and -infinity; all keys where it is not causal."""
+    run([7, 2, 3, 1], [4, 0, -5, 9], 4, 2, 64, 8, window=window, seed=1)
+    run([7, 2, 3, 1], [4, 0, -5, 9], 4, 2, 64, 8, window=window, causal=False, seed=1)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 5.0, 1e-30])
+def test_scales(scale):
+    run([2], [90], 2, 1, 64, 16, name="f32", scale=scale, seed=2)
+
+
+def test_long_sequences_are_cut_and_joined():
+    """Runs of many workgroups, one sequence of which is much longer than the others."""
+    run([1, 1, 1], [20000, 5, 700], 4, 1, 64, 64, "fp4", "fp8", seed=3)
+    run([3], [9000], 8, 2, 256, 64, "fp8", "fp8", "f16", seed=4)
+
+
+@pytest.mark.parametrize("seqs", [64, 65, 256, 257, 600])
+def test_many_sequences(seqs):
+    rng = np.random.default_rng(seqs)
+    new = rng.integers(0, 3, seqs)
+    run(list(new), list(new + rng.integers(0, 40, seqs)), 2, 1, 32, 16, seed=seqs)
+
+
+def test_strides():
+    """Queries inside the result of one product, and heads first; addresses off 16 bytes."""
+    rng = np.random.default_rng(5)
+    table, lengths, offsets, pages = layout([11, 2], [30, 8], 16)
+    cache, keys, values = random_cache(rng, pages, 2, 16, 72, "fp8", "fp8")
+    where = on_gpu(table, lengths, offsets)
+    x = torch.from_numpy(rng.standard_normal((13, 8, 77))).to(torch.bfloat16).to(DEV)
+    q = x[:, 2:6, 5:77]
+    want = hago.mx_attention(q.contiguous(), cache, *where)
+    assert torch.equal(hago.mx_attention(q, cache, *where), want)
+    assert torch.equal(hago.mx_attention(q.transpose(0, 1).contiguous().transpose(0, 1), cache, *where), want)
+    check_attention(want, "bf16", q.double().cpu().numpy(), keys, values, ref.Sequences(table, lengths, offsets, pages, 16), 72 ** -0.5)
+
+
+@pytest.mark.parametrize("k_fmt,v_fmt", [("fp8", "fp8"), ("fp4", "fp4")])
+@pytest.mark.parametrize("dim", [40, 128, 256])
+@pytest.mark.parametrize("new", [4, 150])
+def test_what_is_hidden_is_not_seen(new, dim, k_fmt, v_fmt):
+    """Bytes that nobody wrote, blocks of NaN behind the last token and in tokens that a row does not see: nothing of them reaches it.  A row that sees a block of
+    NaN among its values is NaN in those columns; among its keys, in all."""
+    rng = np.random.default_rng(dim)
+    length, page = 200, 16
+    table, lengths, offsets, pages = layout([new], [length], page)
+    cache, keys, values = random_cache(rng, pages, 1, page, dim, k_fmt, v_fmt)
+    seqs = ref.Sequences(table, lengths, offsets, pages, page)
+    live = torch.zeros(pages, page, dtype=torch.bool)
+    for j in range(length):
+        live[seqs.place(0, j)] = True
+    live = live.to(DEV)[:, None]
+    for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales):
+        t[~live.expand(t.shape[:3])] = 0xFF
+    q = torch.from_numpy(rng.standard_normal((new, 2, dim))).to(torch.bfloat16)
+    where = on_gpu(table, lengths, offsets)
+    want = hago.mx_attention(q.to(DEV), cache, *where)
+    check_attention(want, "bf16", q.double().numpy(), keys, values, seqs, dim ** -0.5)
+    block = (dim - 1) // 32
+    # the values of the last token's last block: the last row alone sees them
+    p, at = seqs.place(0, length - 1)
+    was = cache.v_scales[p, 0, at, block].item(), cache.v_codes[p, 0, at].clone()
+    cache.v_scales[p, 0, at, block] = 255
+    got = hago.mx_attention(q.to(DEV), cache, *where)
+    assert torch.equal(got[:-1], want[:-1])
+    assert got[-1, :, 32 * block:].isnan().all() and torch.equal(got[-1, :, :32 * block], want[-1, :, :32 * block])
+    cache.v_scales[p, 0, at, block] = was[0]
+    # its keys
+    cache.k_scales[p, 0, at, 0] = 255
+    got = hago.mx_attention(q.to(DEV), cache, *where)
+    assert torch.equal(got[:-1], want[:-1]) and got[-1].isnan().all()
+    # a token in the middle, with a window that leaves it to some rows
+    cache.k_scales[p, 0, at, 0] = 127
+    p, at = seqs.place(0, length - 3)
+    cache.v_scales[p, 0, at, 0] = 255
+    got = hago.mx_attention(q.to(DEV), cache, *where, window=2)
+    nan = got.isnan()[..., :32].any(-1).any(-1)
+    assert nan.nonzero().flatten().tolist() == [new - 3, new - 2]
+
+
+def test_pages_that_are_gone():
+    """Entries that are no page: their keys are not there, whatever the window says."""
+    rng = np.random.default_rng(7)
+    table, lengths, offsets, pages = layout([3, 20], [120, 90], 16)
+    cache, keys, values = random_cache(rng, pages, 2, 16, 64, "fp8", "fp8")
+    table[0, :3] = [-1, pages, 2 ** 31 - 1]
+    table[1, 2] = -2 ** 31
+    q = torch.from_numpy(rng.standard_normal((23, 4, 64))).to(torch.bfloat16)
+    where = on_gpu(table, lengths, offsets)
+    seqs = ref.Sequences(table, lengths, offsets, pages, 16)
+    check_attention(hago.mx_attention(q.to(DEV), cache, *where), "bf16", q.double().numpy(), keys, values, seqs, 0.125)
+    table[:] = -1
+    out, lse = hago.mx_attention(q.to(DEV), cache, *on_gpu(table, lengths, offsets), lse=True)
+    assert (out == 0).all() and lse.isneginf().all()
+    # lengths beyond what the table holds
+    table, lengths, offsets, pages = layout([4], [64], 16, extra=0)
+    cache, keys, values = random_cache(rng, pages, 2, 16, 64, "fp8", "fp8")
+    lengths[:] = 66
+    out = hago.mx_attention(q[:4].to(DEV), cache, *on_gpu(table, lengths, offsets))
+    check_attention(out, "bf16", q[:4].double().numpy(), keys, values, ref.Sequences(table, lengths, offsets, pages, 16), 0.125)
+    lengths[:] = 2 ** 31 - 1
+    out = hago.mx_attention(q[:4].to(DEV), cache, *on_gpu(table, lengths, offsets), causal=False)
+    check_attention(out, "bf16", q[:4].double().numpy(), keys, values, ref.Sequences(table, np.array([64]), offsets, pages, 16), 0.125, causal=False)
+
+
+def test_offsets_that_break_the_contract():
+    """Nothing out of range is touched, and every call ends."""
+    rng = np.random.default_rng(8)
+    cache, _, _ = random_cache(rng, 6, 1, 16, 64, "fp8", "fp8")
+    q = torch.randn(12, 2, 64, device=DEV, dtype=torch.bfloat16)
+    table = np.arange(6, dtype=np.int32).reshape(2, 3)
+    for offsets in ([5, 3, 1], [-7, 2 ** 31 - 1, 4], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 12, -12], [-2 ** 31, 12, 12]):
+        for lengths in ([40, 40], [2 ** 31 - 1, -2 ** 31]):
+            hago.mx_attention(q, cache, *on_gpu(table, np.array(lengths, np.int32), np.array(offsets, np.int32)))
+    torch.cuda.synchronize()
+
+
+def test_nothing_to_do():
+    cache = hago.MXCache.empty(2, 1, 4, 32)
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device=DEV)  # noqa: E731
+    assert hago.mx_attention(torch.zeros(0, 2, 32, device=DEV), cache, i(1, 2), i(1), i(2)).shape == (0, 2, 32)
+    out = torch.full((3, 2, 32), 7.0, device=DEV)
+    hago.mx_attention(out * 0, cache, i(0, 2), i(0), i(1), out=out)
+    hago.mx_attention(out * 0, cache, i(2, 2), i(2), i(3), out=out)
+    assert (out == 7).all()
+    no_pages = hago.MXCache.empty(0, 1, 4, 32)
+    hago.mx_attention(out * 0, no_pages, i(1, 2), i(1) + 3, torch.tensor([0, 3], dtype=torch.int32, device=DEV), out=out)
+    assert (out == 0).all()
+
+
+def test_prepared_calls_streams_and_graphs():
+    """The same call on another stream, prepared, and captured twice, both graphs replayed with other lengths and queries; every result is the eager one."""
+    rng = np.random.default_rng(9)
+    table, lengths, offsets, pages = layout([1, 2, 4], [3000, 40, 600], 16, extra=8)
+    cache, _, _ = random_cache(rng, pages, 2, 16, 128, "fp8", "fp4")
+    table, n, o = on_gpu(table.clip(0, pages - 1), lengths, offsets)
+    q = torch.randn(7, 8, 128, device=DEV, dtype=torch.bfloat16)
+    want = hago.mx_attention(q, cache, table, n, o).clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        assert torch.equal(hago.mx_attention(q, cache, table, n, o), want)
+        call = hago.mx_attention(q, cache, table, n, o, prepare=True)
+        assert torch.equal(call(), want)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for scale in (0.05, 0.2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(hago.mx_attention(q, cache, table, n, o, scale=scale))
+        graphs.append(g)
+    for turn in range(3):
+        q.normal_()
+        n.add_(1)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[0].replay()
+        graphs[1].replay()   # at the same time: each has a workspace of its own
+        torch.cuda.synchronize()
+        for scale, out in zip((0.05, 0.2), outs):
+            assert torch.equal(out, hago.mx_attention(q, cache, table, n, o, scale=scale))
+
+
+def test_a_workspace_of_any_contents():
+    rng = np.random.default_rng(10)
+    table, lengths, offsets, pages = layout([1, 5], [2000, 300], 16)
+    cache, _, _ = random_cache(rng, pages, 1, 16, 64, "fp8", "fp8")
+    where = on_gpu(table, lengths, offsets)
+    q = torch.randn(6, 4, 64, device=DEV, dtype=torch.float16)
+    want = hago.mx_attention(q, cache, *where)
+    for byte in (0, 0x7F, 0xFF):
+        room = torch.full((hago.mx_attention_workspace_bytes(6, 4, 1, 64),), byte, dtype=torch.uint8, device=DEV)
+        assert torch.equal(hago.mx_attention(q, cache, *where, workspace=room), want)
+
+
+def test_a_prompt_in_chunks_and_tokens():
+    """The operators together: rotary positions, cache and attention of two prompts at once, in chunks, and token by token.  Every row is the same sum over
+    the same codes, in another order."""
+    torch.manual_seed(0)
+    heads, kv_heads, dim, page, total = 6, 2, 64, 16, 75
+    pages = 2 * -(-total // page)
+    x = torch.randn(2, total, heads + 2 * kv_heads, dim, device=DEV).to(torch.bfloat16)
+    freq = torch.pow(10000.0, -torch.arange(dim // 2, device=DEV) / (dim // 2)).float()
+    table = torch.randperm(pages, device=DEV).to(torch.int32).view(2, -1)
+
+    def serve(cuts):
+        cache = hago.MXCache.empty(pages, kv_heads, page, dim, hago.MX_FP8, hago.MX_FP4)
+        outs = []
+        for first, end in zip(cuts, cuts[1:]):
+            n = end - first
+            qkv = x[:, first:end].reshape(2 * n, -1, dim).clone()
+            positions = torch.arange(first, end, device=DEV, dtype=torch.int32).repeat(2)
+            hago.rope(qkv[:, :heads + kv_heads], positions, freq, out=qkv[:, :heads + kv_heads])
+            lengths = torch.tensor([end, end], dtype=torch.int32, device=DEV)
+            offsets = torch.tensor([0, n, 2 * n], dtype=torch.int32, device=DEV)
+            hago.mx_cache_write(cache, qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:], table, lengths, offsets)
+            outs.append(hago.mx_attention(qkv[:, :heads], cache, table, lengths, offsets).view(2, n, heads, dim))
+        return torch.cat(outs, 1).float(), cache
+    whole, cache = serve([0, total])
+    # what the whole should be, from the values in the cache
+    offsets = torch.tensor([0, total, 2 * total], dtype=torch.int32, device=DEV)
+    k, v = hago.mx_cache_read(cache, table, torch.tensor([total] * 2, dtype=torch.int32, device=DEV), offsets, 2 * total, out_dtype=hago.F32)
+    k, v = (t.view(2, total, kv_heads, 1, dim).expand(2, total, kv_heads, heads // kv_heads, dim).reshape(2, total, heads, dim).transpose(1, 2).double() for t in (k, v))
+    q = hago.rope(x[:, :, :heads].reshape(-1, heads, dim), torch.arange(total, device=DEV, dtype=torch.int32).repeat(2), freq).view(2, total, heads, dim).transpose(1, 2).double()
+    score = (q.unsqueeze(3) * k.unsqueeze(2)).sum(-1) * dim ** -0.5
+    p = score.masked_fill(torch.ones(total, total, dtype=torch.bool, device=DEV).triu(1), -float("inf")).softmax(-1)
+    want = (p.unsqueeze(-1) * v.unsqueeze(2)).sum(3).transpose(1, 2)
+    # 2^-8 for the probabilities, as much for the result, and a thousandth of that for the rest, of sums of at most the values' size
+    limit = 2.02 * 2.0 ** -8 * (p.unsqueeze(-1) * v.abs().unsqueeze(2)).sum(3).transpose(1, 2)
+    for cuts in ([0, total], [0, 1, 2, 30, total], list(range(total + 1))):
+        got, _ = serve(cuts)
+        assert ((got.double() - want).abs() <= limit).all()

@@ -1,0 +1,95 @@
+"""Rotary positions on the GPU against the oracle in 64 bits.
+
+Cosine and sine come from a binary64 angle, whose fraction of a turn is rounded to binary32 (2^-24 of at most pi / 4) and goes through two
+polynomials (less than 2^-23 in all); two products, a fused sum (2^-24 each) and the result's own rounding.  The whole is below
+`4 * 2^-23 * (|a| + |b|)` and half a step of the type."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2103_14949_amd as hago
+from oracle import cache_ref as ref
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def inputs(T, heads, dim, pairs, axes, dtype, seed, far=5000):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, heads, dim, generator=g).to(dtype)
+    pos = torch.randint(0, far, (axes, T), generator=g, dtype=torch.int32)
+    freq = torch.pow(10000.0, -torch.arange(pairs) / max(pairs, 1)).float()
+    axis = torch.randint(0, axes, (pairs,), generator=g, dtype=torch.int32) if axes > 1 else None
+    return x, pos, freq, axis
+
+
+def check(got, x, pos, freq, axis, interleaved, name):
+    want = ref.rope(x.double().numpy(), pos.numpy(), freq.numpy(), None if axis is None else axis.numpy(), interleaved)
+    pairs = len(freq)
+    size = x.double().abs().numpy()
+    a, b = (slice(0, 2 * pairs, 2), slice(1, 2 * pairs, 2)) if interleaved else (slice(0, pairs), slice(pairs, 2 * pairs))
+    bound = np.zeros_like(want)
+    bound[..., a] = bound[..., b] = 4 * 2.0 ** -23 * (size[..., a] + size[..., b])
+    bound = bound * 1.01 + torch.finfo(TYPES[name]).eps / 2 * np.abs(want) + (2.0 ** -25 if name == "f16" else 0)
+    bound[..., 2 * pairs:] = 0
+    got = got.double().cpu().numpy()
+    assert (np.abs(got - want) <= bound).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,heads,dim,pairs,axes", [(1, 1, 2, 1, 1), (1, 40, 128, 64, 1), (3, 5, 7, 3, 2), (17, 3, 80, 33, 3), (5, 2, 64, 8, 1), (9, 1, 33, 16, 3),
+                                                    (70, 4, 256, 128, 2), (2, 3, 96, 0, 1), (4, 2, 40, 5, 4), (1100, 2, 18, 9, 1), (2, 1, 4096, 2048, 2)])
+def test_sizes(T, heads, dim, pairs, axes, name, interleaved):
+    x, pos, freq, axis = inputs(T, heads, dim, pairs, axes, TYPES[name], T + dim)
+    got = hago.rope(x.to(DEV), pos.to(DEV), freq.to(DEV), axes=None if axis is None else axis.to(DEV), interleaved=interleaved)
+    assert got.dtype == x.dtype and got.is_contiguous()
+    check(got, x, pos, freq, axis, interleaved, name)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_far_positions(interleaved):
+    """Positions up to the last one: the angle keeps its fraction."""
+    x, pos, freq, _ = inputs(64, 2, 64, 32, 1, torch.float32, 3)
+    pos = torch.randint(2 ** 30, 2 ** 31 - 1, (64,), dtype=torch.int32, generator=torch.Generator().manual_seed(1))
+    pos[:3] = torch.tensor([2 ** 31 - 1, -(2 ** 31), -1])
+    got = hago.rope(x.to(DEV), pos.to(DEV), freq.to(DEV), interleaved=interleaved)
+    check(got, x, pos[None], freq, None, interleaved, "f32")
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("name,offset", [("bf16", 0), ("bf16", 1), ("f32", 1), ("f16", 3)])
+def test_strides_and_places(name, offset, interleaved):
+    """Parts of a product's result, heads-first tensors, addresses off 16 bytes; in place, and into a larger tensor whose rest stays."""
+    x, pos, freq, _ = inputs(19, 12, 52, 23, 1, TYPES[name], 5)
+    dev = torch.empty(x.numel() + offset, dtype=x.dtype, device=DEV)[offset:].view(x.shape)
+    dev.copy_(x)
+    p, f = pos.to(DEV), freq.to(DEV)
+    part = dev[:, 3:8, :50]
+    got = hago.rope(part, p, f, interleaved=interleaved)
+    check(got, x[:, 3:8, :50], pos, freq, None, interleaved, name)
+    first = dev.transpose(0, 1).contiguous().transpose(0, 1)   # [heads, T, dim] in memory
+    check(hago.rope(first, p, f, interleaved=interleaved, out=torch.empty_like(first)), x, pos, freq, None, interleaved, name)
+    assert hago.rope(part, p, f, interleaved=interleaved, out=part) is part
+    assert torch.equal(dev[:, 3:8, :50], got)
+    rest = dev.clone().cpu()
+    rest[:, 3:8, :50] = x[:, 3:8, :50]
+    assert torch.equal(rest, x)
+
+
+def test_empty_and_prepared():
+    x, pos, freq, _ = inputs(6, 2, 32, 16, 1, torch.bfloat16, 1)
+    assert hago.rope(x[:0].to(DEV), pos[:, :0].contiguous().to(DEV), freq.to(DEV)).shape == (0, 2, 32)
+    d = x.to(DEV)
+    call = hago.rope(d, pos.to(DEV), freq.to(DEV), prepare=True)
+    d.neg_()
+    check(call(), -x, pos, freq, None, False, "bf16")
+
+
+def test_an_axis_that_is_none_has_position_zero():
+    x, pos, freq, _ = inputs(4, 2, 8, 4, 2, torch.float32, 2)
+    axis = torch.tensor([0, 1, 2, -1], dtype=torch.int32)
+    got = hago.rope(x.to(DEV), pos.to(DEV), freq.to(DEV), axes=axis.to(DEV))
+    assert torch.equal(got[..., [2, 3, 6, 7]].cpu(), x[..., [2, 3, 6, 7]])
