@@ -16,122 +16,11 @@ namespace hago {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kKeys = 32, kBlock = kWaves * kKeys;
+constexpr int kThreads = 256, kWaves = 4, kRows = 16, kKeys = 32, kBlock = kWaves * kKeys;
 // Workgroups that share the keys, by blocks of a row: as many as are resident.
 template <int DB>
 constexpr int kRuns = DB == 8 ? 512 : 1024;
 constexpr int kMostRuns = 1024;
-
-struct AttentionWork {
-  float* partial;   // [2 kRuns][16][32 DB]
-  float2* stats;    // [2 kRuns][16]: maximum and sum
-  int2* joins;      // [T][heads]: 16 * first partial + row, number of partials
-};
-
-__device__ __forceinline__ int64_t scan_within_block(int64_t v, int64_t* totals, int64_t& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  int64_t sum = v;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t other = __shfl_up(sum, d);
-    if (lane >= d) sum += other;
-  }
-  if (lane == 63) totals[wave] = sum;
-  __syncthreads();
-  total = 0;
-  int64_t before = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += totals[w];
-    total += totals[w];
-  }
-  __syncthreads();
-  return before + sum - v;
-}
-
-// A workgroup's run.
-struct Run {
-  int seq, local, runs, slot;  // place among the sequence's runs, runs of a unit, first partial of the sequence (-1: none)
-};
-
-// Units are (16 rows, head); each is cut into ceil(blocks / share) runs.
-__device__ __forceinline__ bool find_run(const CacheArgs& c, const AttentionArgs& a, int group, int share_of, int64_t id, Run& run) {
-  __shared__ int64_t totals[kWaves];
-  __shared__ Run found;
-  const int tid = threadIdx.x;
-  const auto sizes = [&](int s, int64_t& units, int64_t& blocks) {
-    units = 0, blocks = 0;
-    if (s >= c.seqs) return;
-    const AttentionSpan span = attention_span(c, a, s);
-    units = ((int64_t)span.rows * group + 15) / 16 * c.kv_heads;
-    blocks = span.high > span.low ? (span.high - (span.low & ~15) + kBlock - 1) / kBlock : 1;
-  };
-  int64_t units, blocks, all = 0;
-  for (int s = 0; s < c.seqs; s += kThreads) {
-    int64_t total;
-    sizes(s + tid, units, blocks);
-    scan_within_block(units * blocks, totals, total);
-    all += total;
-  }
-  const int64_t share = all > share_of ? (all + share_of - 1) / share_of : 1;
-  if (tid == 0) found.seq = -1;
-  int64_t before = 0, slots_before = 0;
-  for (int s = 0; s < c.seqs; s += kThreads) {
-    if (c.seqs > kThreads) sizes(s + tid, units, blocks);
-    const int64_t runs = (blocks + share - 1) / share;
-    // (both counts below 2^31)
-    int64_t total;
-    const int64_t at = scan_within_block(units * runs << 32 | (runs > 1 ? units * runs : 0), totals, total);
-    const int64_t first = before + (at >> 32);
-    if (id >= first && id < first + units * runs)
-      found = Run{s + tid, (int)(id - first), (int)runs, runs > 1 ? (int)(slots_before + (at & 0xffffffff)) : -1};
-    before += total >> 32;
-    slots_before += total & 0xffffffff;
-    if (before > id) break;
-  }
-  __syncthreads();
-  run = found;
-  // (the same in all lanes, which the compiler does not know of what lies in LDS)
-  run.seq = __builtin_amdgcn_readfirstlane(run.seq);
-  run.local = __builtin_amdgcn_readfirstlane(run.local);
-  run.runs = __builtin_amdgcn_readfirstlane(run.runs);
-  run.slot = __builtin_amdgcn_readfirstlane(run.slot);
-  return run.seq >= 0;
-}
-
-// A lane's part of a key or value: 8 DB codes.
-template <int FORMAT, int DB>
-struct Chunk {
-  static constexpr int kWords = FORMAT == kMxFp4 ? DB : 2 * DB;
-  static constexpr int kScales = DB == 8 ? 2 : 1;
-  static constexpr int kRowWords = FORMAT == kMxFp4 ? 4 : 8;  // of a block
-  static constexpr int kPiece = kWords < 4 ? kWords : 4;      // of a load
-  uint32_t w[kWords];
-  uint32_t scale[kScales];
-
-  // Of any row that there is.  Where a row has fewer blocks than DB, the pieces behind its end are others of its own: queries are zero there, and
-  // results are not kept.
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t place, int blocks, int part) {
-    typedef uint32_t piece __attribute__((ext_vector_type(kPiece)));
-    const uint32_t* row = reinterpret_cast<const uint32_t*>(codes) + place * (blocks * kRowWords);
-#pragma unroll
-    for (int i = 0; i < kWords; i += kPiece) {
-      const int at = part * kWords + i, most = blocks * kRowWords - kPiece;
-      const piece p = *reinterpret_cast<const piece*>(row + (at < most ? at : most));
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k) w[i + k] = p[k];
-    }
-#pragma unroll
-    for (int i = 0; i < kScales; ++i) {
-      const int block = part * DB / 4 + i;
-      scale[i] = scales[place * blocks + (block < blocks ? block : blocks - 1)];
-    }
-  }
-  // eight codes of step st
-  __device__ __forceinline__ at_b8 values(int st) const {
-    return attention_values8<FORMAT>(w + st * (FORMAT == kMxFp4 ? 1 : 2), __builtin_bit_cast(float, scale[st / 4 % kScales] << 23));
-  }
-};
 
 __device__ __forceinline__ float max_of_parts(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
@@ -152,8 +41,8 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   static_assert(16 * kSums * 4 + 128 <= kRegion);
   __shared__ __align__(16) uint8_t lds[kWaves * kRegion];
 
-  Run run;
-  if (!find_run(c, a, group, kRuns<DB>, blockIdx.x, run)) return;
+  AttentionRun run;
+  if (!attention_run<kThreads, kRows, kBlock>(c, a, group, kRuns<DB>, blockIdx.x, run)) return;
   const AttentionSpan span = attention_span(c, a, run.seq);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, part = lane / 16;
   const int tiles = (int)(((int64_t)span.rows * group + 15) / 16);
@@ -209,8 +98,8 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   uint8_t* mine = lds + wave * kRegion;
   float m = -INFINITY, l = 0.0f;
   at_f4 o[2 * DB] = {};
-  Chunk<KF, DB> kc[2];
-  Chunk<VF, DB> vc[2];
+  AttentionChunk<KF, DB> kc[2];
+  AttentionChunk<VF, DB> vc[2];
   bool there[2];  // the key has a place
   const auto load = [&](int base) {
 #pragma unroll
@@ -228,7 +117,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   for (; base < k1; base += kBlock) {
     // S^T, values into LDS
     at_f4 s[2] = {};
-    uint64_t none[2][Chunk<VF, DB>::kScales];  // lanes whose blocks of a value stand for NaN
+    uint64_t none[2][AttentionChunk<VF, DB>::kScales];  // lanes whose blocks of a value stand for NaN
     uint32_t seen = ((uint32_t)__ballot(there[0]) & 0xffff) | (uint32_t)__ballot(there[1]) << 16;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -239,7 +128,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
         for (int p = PIECES - 1; p >= 0; --p) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][st], s[i], 0, 0, 0);
       }
       // (what has no place, and what is NaN, is zero here: a probability of zero does not take a NaN away)
-      constexpr int kScales = Chunk<VF, DB>::kScales, kEach = Chunk<VF, DB>::kWords / kScales;
+      constexpr int kScales = AttentionChunk<VF, DB>::kScales, kEach = AttentionChunk<VF, DB>::kWords / kScales;
 #pragma unroll
       for (int b = 0; b < kScales; ++b) {
         const bool nan = vc[i].scale[b] == 255, zero = nan || !there[i];
@@ -299,7 +188,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
     }
     uint64_t any = 0;
 #pragma unroll
-    for (int b = 0; b < Chunk<VF, DB>::kScales; ++b) any |= none[0][b] | none[1][b];
+    for (int b = 0; b < AttentionChunk<VF, DB>::kScales; ++b) any |= none[0][b] | none[1][b];
     if (any) {
       // NaN for the queries that see such a value, and for no other: tile d is columns 16 d on, which part 2 d / DB holds
 #pragma unroll
@@ -363,9 +252,9 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   }
 }
 
-// Joins the runs of a row.  Four columns a thread, the runs by turns; the order of the sums is the runs'.
+// Joins the runs of a row, whose partials are `apart` rows apart.  Four columns a thread, the runs by turns; the order of the sums is the runs'.
 template <int TYPE, int DB>
-__global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int64_t rows) {
+__global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int64_t rows, int apart, int slots) {
   using E = typename MxElement<TYPE>::type;
   constexpr int D = 32 * DB, kColumns = D / 4, kTurns = kThreads / kColumns;
   __shared__ float weights[kMostRuns];
@@ -378,9 +267,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
     const int2 join = work.joins[row];
     const int runs = join.y;
     // (what no sequence wrote may be anything)
-    if (runs < 2 || runs > kRuns<DB> || join.x < 0 || (int64_t)join.x + 16 * (runs - 1) >= 32 * kRuns<DB>) continue;
+    if (runs < 2 || runs > kMostRuns || join.x < 0 || (int64_t)join.x + (int64_t)apart * (runs - 1) >= (int64_t)apart * slots) continue;
     float most = -INFINITY, sum = 0.0f;
-    for (int i = tid; i < runs; i += kThreads) most = fmaxf(most, work.stats[join.x + 16 * i].x);
+    for (int i = tid; i < runs; i += kThreads) most = fmaxf(most, work.stats[join.x + (int64_t)apart * i].x);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
     __syncthreads();
@@ -389,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
     most = fmaxf(fmaxf(shared[0][0], shared[1][0]), fmaxf(shared[2][0], shared[3][0]));
     const float zero = most == -INFINITY ? 0.0f : most;
     for (int i = tid; i < runs; i += kThreads) {
-      const float2 s = work.stats[join.x + 16 * i];
+      const float2 s = work.stats[join.x + (int64_t)apart * i];
       const float w = __builtin_amdgcn_exp2f(s.x - zero);
       weights[i] = w;
       sum = __builtin_fmaf(s.y, w, sum);
@@ -402,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
     const int col = tid % kColumns, turn = tid / kColumns;
     at_f4 y = {};
     for (int i = turn; i < runs; i += kTurns) {
-      const at_f4 p = *reinterpret_cast<const at_f4*>(work.partial + ((int64_t)join.x + 16 * i) * D + 4 * col);
+      const at_f4 p = *reinterpret_cast<const at_f4*>(work.partial + (join.x + (int64_t)apart * i) * D + 4 * col);
 #pragma unroll
       for (int k = 0; k < 4; ++k) y[k] = __builtin_fmaf(p[k], weights[i], y[k]);
     }
@@ -423,23 +312,31 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
   }
 }
 
-constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }
-int blocks_of(int64_t dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
-int64_t partial_floats(int db) { return 2ll * (db == 8 ? kRuns<8> : kRuns<4>) * 16 * 32 * db; }
-int64_t stats_bytes(int db) { return 2ll * (db == 8 ? kRuns<8> : kRuns<4>) * 16 * (int64_t)sizeof(float2); }
+// Which kernel: the one for many rows where a sequence has this many on the average, queries of all heads that share keys.
+constexpr int64_t kManyRowsFrom = 64;
+bool many_rows(const AttentionArgs& a, const CacheArgs& c) { return (int64_t)a.T * (a.heads / c.kv_heads) >= kManyRowsFrom * c.seqs; }
 
+constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }
+
+template <int TYPE, int DB>
+hipError_t launch_join(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, int apart, int slots, hipStream_t st) {
+  const int64_t rows = (int64_t)a.T * a.heads, most = max_blocks(kThreads);
+  return launch_kernel(join_kernel<TYPE, DB>, dim3((uint32_t)(rows < most ? rows : most)), dim3(kThreads), 0, st, c, a, work, rows, apart, slots);
+}
 template <int TYPE, int KF, int VF, int DB>
 hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
   const int group = a.heads / c.kv_heads;
-  const int64_t units = ((int64_t)a.T * group / 16 + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
+  if (TYPE == kMxBf16 && many_rows(a, c)) {
+    const hipError_t e = launch_attention_many(c, a, work, st);
+    return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(DB), 2 * kAttentionManyRuns, st);
+  }
+  const int64_t units = ((int64_t)a.T * group / kRows + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
   const hipError_t e = launch_kernel(attention_kernel<TYPE, KF, VF, DB>, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, group);
-  if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)a.T * a.heads, most = max_blocks(kThreads);
-  return launch_kernel(join_kernel<TYPE, DB>, dim3((uint32_t)(rows < most ? rows : most)), dim3(kThreads), 0, st, c, a, work, rows);
+  return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, kRows, 2 * kRuns<DB>, st);
 }
 template <int TYPE, int KF, int VF>
 hipError_t with_dim(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
-  switch (blocks_of(c.dim)) {
+  switch (attention_blocks(c.dim)) {
     case 2: return launch<TYPE, KF, VF, 2>(c, a, work, st);
     case 4: return launch<TYPE, KF, VF, 4>(c, a, work, st);
   }
@@ -453,18 +350,26 @@ hipError_t with_formats(const CacheArgs& c, const AttentionArgs& a, const Attent
 
 }  // namespace
 
+// Rows of partials that a call can have.
+static int64_t partial_rows(int64_t T, int64_t heads, int64_t kv_heads, int db) {
+  const int64_t few = 2ll * (db == 8 ? kRuns<8> : kRuns<4>) * kRows;
+  const int64_t many = 2ll * kAttentionManyRuns * attention_many_rows(db);
+  return T * (heads / kv_heads) >= kManyRowsFrom && many > few ? many : few;
+}
+
 int64_t mx_attention_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t dim) {
-  const int db = blocks_of(dim);
-  return partial_floats(db) * 4 + stats_bytes(db) + padded16(T * heads * (int64_t)sizeof(int2));
+  const int db = attention_blocks(dim);
+  return partial_rows(T, heads, kv_heads, db) * (32 * db * 4 + (int64_t)sizeof(float2)) + padded16(T * heads * (int64_t)sizeof(int2));
 }
 
 hipError_t launch_mx_attention(const CacheArgs& c, const AttentionArgs& a, void* workspace, hipStream_t st) {
-  const int db = blocks_of(c.dim);
+  const int db = attention_blocks(c.dim);
+  const int64_t rows = partial_rows(a.T, a.heads, c.kv_heads, db);
   uint8_t* w = static_cast<uint8_t*>(workspace);
   AttentionWork work;
   work.partial = reinterpret_cast<float*>(w);
-  work.stats = reinterpret_cast<float2*>(w + partial_floats(db) * 4);
-  work.joins = reinterpret_cast<int2*>(w + partial_floats(db) * 4 + stats_bytes(db));
+  work.stats = reinterpret_cast<float2*>(w + rows * 32 * db * 4);
+  work.joins = reinterpret_cast<int2*>(w + rows * (32 * db * 4 + (int64_t)sizeof(float2)));
   return a.type == kMxF32 ? with_formats<kMxF32>(c, a, work, st) : a.type == kMxBf16 ? with_formats<kMxBf16>(c, a, work, st) : with_formats<kMxF16>(c, a, work, st);
 }
 
