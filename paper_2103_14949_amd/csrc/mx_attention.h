@@ -185,10 +185,8 @@ struct AttentionChunk {
 // Host side: blocks of 32 columns that the kernels are made for, and what the kernel for many rows has of rows and runs.
 constexpr int attention_blocks(int64_t dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
 template <int DB>
-constexpr int kManyGroups = DB == 8 ? 1 : 2;
-template <int DB>
-constexpr int kManyWaves = 4;
-constexpr int attention_many_rows(int db) { return db == 2 ? 32 * kManyGroups<2> * kManyWaves<2> : db == 4 ? 32 * kManyGroups<4> * kManyWaves<4> : 32 * kManyGroups<8> * kManyWaves<8>; }
+constexpr int kManyWaves = DB == 8 ? 4 : 8;
+constexpr int attention_many_rows(int db) { return 32 * (db == 2 ? kManyWaves<2> : db == 4 ? kManyWaves<4> : kManyWaves<8>); }
 constexpr int kAttentionManyRuns = 256;
 hipError_t launch_attention_many(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st);
 

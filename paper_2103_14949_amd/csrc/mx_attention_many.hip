@@ -1,7 +1,7 @@
 // Attention over a paged cache of microscaled keys and values, many rows a sequence: chunks and prompts.
 //
 // The matrix unit bounds it.  A workgroup is one (sequence, tile of rows, head of the cache) and a run of keys; its rows are the queries of all heads
-// that share those keys, 32 or 64 a wavefront.  Keys and values of 64 positions at a time become bfloat16 once for all of them, on their way from
+// that share those keys, 32 a wavefront.  Keys and values of 64 positions at a time become bfloat16 once for all of them, on their way from
 // memory through registers into LDS, two tiles deep with one barrier a tile; the conversions are hidden behind the products.  S^T = K Q^T leaves a
 // query's scores in two lanes' registers, as the operand of O^T = V^T P^T, so that the softmax needs one lane exchange and nothing of it goes
 // through LDS; values are read transposed from there.
@@ -19,22 +19,26 @@ constexpr int kTile = 64;  // keys
 __device__ __forceinline__ float pair_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float pair_sum(float v) { return v + __shfl_xor(v, 32); }
 
-template <int TYPE, int KF, int VF, int DB, int RG, int WAVES>
+template <int TYPE, int KF, int VF, int DB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int group, int share_of, int slots) {
   using E = typename MxElement<TYPE>::type;
-  constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * RG * WAVES, STEPS = 2 * DB;
+  constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * WAVES, STEPS = 2 * DB, kProducts = 2 * STEPS, kAhead = 4;
   constexpr int kKeyRow = 2 * D + 16, kValueRow = 2 * D + 64;  // bytes in LDS: neighbours on different banks, as they are read
-  constexpr int kLoaders = 256;                                // threads that load a tile's keys, and its values
-  using KeyChunk = AttentionChunk<KF, DB>;
-  using ValueChunk = AttentionChunk<VF, DB>;
-  struct Buffer {
-    uint8_t keys[kTile * kKeyRow];
-    uint8_t values[kTile * kValueRow];
-    uint64_t none[2][4];  // bit 4 (key % 16) + part of [block of the part][key / 16]: a value's block that stands for NaN
-    uint64_t gone[4];     // the key has no place
+  constexpr int PARTS = THREADS / kTile, kChunk = 4 * DB / PARTS;   // threads that load a key, and a value
+  constexpr int kKeysAWave = 64 / PARTS;
+  using KeyChunk = AttentionChunk<KF, kChunk>;
+  using ValueChunk = AttentionChunk<VF, kChunk>;
+  struct Values {
+    uint8_t rows[kTile * kValueRow];
+    uint64_t none[ValueChunk::kScales][WAVES];  // bit PARTS * (key % kKeysAWave) + part: the part's block of a value stands for NaN
+    uint64_t gone[WAVES];  // the key has no place
+  };
+  struct Shared {
+    uint8_t keys[2][kTile * kKeyRow];
+    Values values[2];
   };
   extern __shared__ __align__(16) uint8_t lds[];
-  Buffer* const buffers = reinterpret_cast<Buffer*>(lds);
+  Shared& shared = *reinterpret_cast<Shared*>(lds);
 
   AttentionRun run;
   if (!attention_run<THREADS, ROWS, kTile>(c, a, group, share_of, blockIdx.x, run)) return;
@@ -56,34 +60,28 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
     return p < 0 ? 0 : p < span.high ? (int)p : span.high;
   };
 
-  // this lane's queries
-  at_b8 q[RG][PIECES][STEPS];
-  int low[RG], end[RG];
+  // this lane's query
+  at_b8 q[PIECES][STEPS];
+  const int64_t index = (int64_t)tile * ROWS + wave * 32 + (lane & 31);
+  const bool row_there = index < all_rows;
+  const int token = row_there ? (int)(index / group) : 0;
+  const int q_head = head * group + (row_there ? (int)(index - (int64_t)token * group) : 0);
+  const int low = row_there ? low_of(token) : 0, end = row_there ? end_of(token) : 0;
 #pragma unroll
-  for (int g = 0; g < RG; ++g) {
-    const int64_t index = (int64_t)tile * ROWS + (wave * RG + g) * 32 + (lane & 31);
-    const bool row_there = index < all_rows;
-    const int token = row_there ? (int)(index / group) : 0;
-    const int64_t t = span.first + token;
-    const int q_head = head * group + (int)(index - (int64_t)token * group);
-    low[g] = row_there ? low_of(token) : 0;
-    end[g] = row_there ? end_of(token) : 0;
+  for (int st = 0; st < STEPS; ++st) {
+    const int col = 16 * st + 8 * half;
+    float x[8];
+    if (row_there && col < c.dim)
+      mx_load8<TYPE>(static_cast<const E*>(a.q.data) + (int64_t)(span.first + token) * a.q.row + (int64_t)q_head * a.q.head + col, c.dim - col, x);
+    else
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      const int col = 16 * st + 8 * half;
-      float x[8];
-      if (row_there && col < c.dim)
-        mx_load8<TYPE>(static_cast<const E*>(a.q.data) + t * a.q.row + (int64_t)q_head * a.q.head + col, c.dim - col, x);
-      else
+      for (int i = 0; i < 8; ++i) x[i] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+    for (int i = 0; i < 8; ++i) {
+      __bf16 p[PIECES];
+      attention_split<PIECES>(a.scale < 0 ? -x[i] : x[i], p);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __bf16 p[PIECES];
-        attention_split<PIECES>(a.scale < 0 ? -x[i] : x[i], p);
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) q[g][k][st][i] = p[k];
-      }
+      for (int k = 0; k < PIECES; ++k) q[k][st][i] = p[k];
     }
   }
 
@@ -96,90 +94,119 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   const int tile_low = low_of((int)((int64_t)tile * ROWS / group)) & ~15, tile_end = end_of((int)(last_row / group));
   if (k0 < tile_low) k0 = tile_low;
   if (k1 > tile_end) k1 = tile_end;
-  const int64_t wave_first = (int64_t)tile * ROWS + wave * RG * 32;
-  const int64_t wave_last = wave_first + RG * 32 - 1 < last_row ? wave_first + RG * 32 - 1 : last_row;
+  const int64_t wave_first = (int64_t)tile * ROWS + wave * 32;
+  const int64_t wave_last = wave_first + 31 < last_row ? wave_first + 31 : last_row;
   const bool wave_there = wave_first <= last_row;
   const int wave_low = wave_there ? low_of((int)(wave_first / group)) : 0, wave_end = wave_there ? end_of((int)(wave_last / group)) : 0;
   // (rows behind the last one see nothing, but nothing of theirs is kept: they may as well see all)
   const int wave_all_low = wave_there ? low_of((int)(wave_last / group)) : 0, wave_all_end = wave_there ? end_of((int)(wave_first / group)) : 0;
 
-  // loaders: four threads a key
-  const int loader = threadIdx.x & (kLoaders - 1), loader_key = loader / 4, part = loader & 3;
-  const bool loads_keys = threadIdx.x < kLoaders, loads_values = WAVES == 4 || !loads_keys;
+  // On their way: the pages of a tile's keys, then its codes, one tile of values and two of keys ahead of the products
+  const int loader_key = threadIdx.x / PARTS, part = threadIdx.x % PARTS;
   int32_t next_page;
   KeyChunk kc;
   ValueChunk vc;
   bool there;
-  const auto look_up = [&](int base) {  // the page of this thread's key of a tile
+  const auto look_up = [&](int base) {
     const int key = base + loader_key;
-    next_page = key < k1 ? c.table[run.seq * c.table_stride + cache_page_of(c, (uint32_t)key)] : -1;
+    next_page = -1;
+    if (key < k1) next_page = c.table[run.seq * c.table_stride + cache_page_of(c, (uint32_t)key)];
   };
-  const auto load = [&](int base) {
+  const auto place_of = [&](int base) {  // (0 where there is none)
     const uint32_t key = base + loader_key;
     there = (uint32_t)next_page < (uint32_t)c.pages;
-    const int64_t place = there ? ((int64_t)next_page * c.kv_heads + head) * c.page + (key - cache_page_of(c, key) * (uint32_t)c.page) : 0;
-    if (loads_keys) kc.load(c.k_codes, c.k_scales, place, blocks, part);
-    if (loads_values) vc.load(c.v_codes, c.v_scales, place, blocks, part);
+    return there ? ((int64_t)next_page * c.kv_heads + head) * c.page + (key - cache_page_of(c, key) * (uint32_t)c.page) : 0;
   };
-  const auto store = [&](Buffer& b) {
-    if (loads_keys) {
+  const auto store_keys = [&](int turn, int st) {
+    *reinterpret_cast<at_b8*>(shared.keys[turn] + loader_key * kKeyRow + part * 16 * kChunk + 16 * st) = kc.values(st);
+  };
+  const auto prepare_values = [&](int turn, bool values_there) {
+    Values& v = shared.values[turn];
+    constexpr int kScales = ValueChunk::kScales, kEach = ValueChunk::kWords / kScales;
 #pragma unroll
-      for (int st = 0; st < DB; ++st) *reinterpret_cast<at_b8*>(b.keys + loader_key * kKeyRow + part * 16 * DB + 16 * st) = kc.values(st);
+    for (int s = 0; s < kScales; ++s) {
+      const bool nan = vc.scale[s] == 255, zero = nan || !values_there;
+      const uint64_t none = __ballot(nan && values_there);
+      if (lane == 0) v.none[s][wave] = none;
+      if (zero) vc.scale[s] = 0;
+#pragma unroll
+      for (int w = 0; w < kEach; ++w) vc.w[s * kEach + w] = zero ? 0 : vc.w[s * kEach + w];
     }
-    if (loads_values) {
-      constexpr int kScales = ValueChunk::kScales, kEach = ValueChunk::kWords / kScales;
-#pragma unroll
-      for (int s = 0; s < kScales; ++s) {
-        const bool nan = vc.scale[s] == 255, zero = nan || !there;
-        const uint64_t none = __ballot(nan && there);
-        if (lane == 0) b.none[s][wave & 3] = none;
-        if (zero) vc.scale[s] = 0;
-#pragma unroll
-        for (int w = 0; w < kEach; ++w) vc.w[s * kEach + w] = zero ? 0 : vc.w[s * kEach + w];
-      }
-      const uint64_t gone = __ballot(!there);
-      if (lane == 0) b.gone[wave & 3] = gone;
-#pragma unroll
-      for (int st = 0; st < DB; ++st) *reinterpret_cast<at_b8*>(b.values + loader_key * kValueRow + part * 16 * DB + 16 * st) = vc.values(st);
-    }
+    const uint64_t gone = __ballot(!values_there);
+    if (lane == 0) v.gone[wave] = gone;
+  };
+  const auto store_values = [&](int turn, int st) {
+    *reinterpret_cast<at_b8*>(shared.values[turn].rows + loader_key * kValueRow + part * 16 * kChunk + 16 * st) = vc.values(st);
   };
 
-  float m[RG], l[RG];
-  at_f16 o[RG][DB];
+  float m = -INFINITY, l = 0.0f, most = -INFINITY;
+  at_f16 o[DB];
 #pragma unroll
-  for (int g = 0; g < RG; ++g) {
-    m[g] = -INFINITY, l[g] = 0.0f;
+  for (int d = 0; d < DB; ++d) o[d] = at_f16{};
+  // S^T: keys 32 i + 8 (e / 4) + 4 half + e % 4 of query lane % 32, element 16 i + e of a lane's 32.
+  struct Scores {
+    at_f16 s[2];
+  };
+  const auto key_of = [&](int turn, int k) {  // operand k of the scores' products
+    return *reinterpret_cast<const at_b8*>(shared.keys[turn] + (32 * (k / STEPS) + (lane & 31)) * kKeyRow + 32 * (k % STEPS) + 16 * half);
+  };
+  const auto score = [&](Scores& s, int k, const at_b8& key) {
+    if (k % STEPS == 0) s.s[k / STEPS] = at_f16{};
 #pragma unroll
-    for (int d = 0; d < DB; ++d) o[g][d] = at_f16{};
-  }
-
-  if (k0 < k1) {
-    look_up(k0);
-    load(k0);
-    look_up(k0 + kTile);
-    store(buffers[0]);
-    load(k0 + kTile);
-    look_up(k0 + 2 * kTile);
-  }
-  __syncthreads();
-  for (int base = k0, turn = 0; base < k1; base += kTile, turn ^= 1) {
-    const Buffer& b = buffers[turn];
-    if (base < wave_end && base + kTile > wave_low) {
-      // S^T: keys 32 i + 8 (e / 4) + 4 half + e % 4 of query lane % 32
-      at_f16 s[RG][2];
+    for (int p = PIECES - 1; p >= 0; --p) s.s[k / STEPS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[p][k % STEPS], s.s[k / STEPS], 0, 0, 0);
+  };
+  const auto value_of = [&](int turn, int k) {  // operand k of the results' products: keys 16 (k / DB) on, columns 32 (k % DB) on
+    union {
+      at_s4 half[2];
+      at_b8 whole;
+    } v;
+    const uint8_t* from = shared.values[turn].rows + (4 * half + (lane & 15) / 4) * kValueRow + 2 * ((lane & 16) + 4 * (lane & 3)) + 16 * (k / DB) * kValueRow + 64 * (k % DB);
+    v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)from);
+    v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)(from + 8 * kValueRow));
+    return v.whole;
+  };
+  const auto most_of = [&](const Scores& s) {
+    float most = s.s[0][0];
 #pragma unroll
-      for (int g = 0; g < RG; ++g) s[g][0] = s[g][1] = at_f16{};
+    for (int e = 1; e < 32; ++e) most = fmaxf(most, s.s[e / 16][e % 16]);
+    return most;
+  };
+  const auto seen_by_wave = [&](int base) { return base < wave_end && base + kTile > wave_low; };
+  const auto all_scores = [&](int turn, Scores& s) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+    for (int k = 0; k < kProducts; ++k) score(s, k, key_of(turn, k));
+  };
+  bool values_there = false, keys_there = false;
+  int64_t value_place = 0;
+  // values of the next tile and keys of the one after it into LDS, those behind them under way; in kForward parts
+  constexpr int kForward = 2 * kChunk + 3;
+  const auto forward = [&](int turn, int base, int k) {
+    if (k == 0) prepare_values(turn ^ 1, values_there);
+    if (k >= 1 && k <= kChunk) store_values(turn ^ 1, k - 1);
+    if (k > kChunk && k <= 2 * kChunk) store_keys(turn, k - 1 - kChunk);
+    if (k == 2 * kChunk + 1) {
+      values_there = keys_there;
+      vc.load(c.v_codes, c.v_scales, value_place, blocks, part);
+    }
+    if (k == 2 * kChunk + 2) {
+      value_place = place_of(base + 3 * kTile);
+      keys_there = there;
+      kc.load(c.k_codes, c.k_scales, value_place, blocks, part);
+      look_up(base + 4 * kTile);
+    }
+  };
+  // Tile `base`, whose scores and their largest are there: its share of the results; and the scores of the next one.  In the order that it is written in
+  // (the fences hold the compiler to it): operands are read kAhead products ahead, the next tile's scores alternate with this one's
+  // exponentials, this one's results with what is under way and the next one's maximum.
+  const auto step = [&](int base, int turn, Scores& s, Scores& next) {
+    const Values& b = shared.values[turn];
+    if (seen_by_wave(base)) {
+      at_b8 keys[kAhead], values[kAhead];
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const at_b8 k = *reinterpret_cast<const at_b8*>(b.keys + (32 * i + (lane & 31)) * kKeyRow + 32 * st + 16 * half);
+      for (int k = 0; k < kAhead; ++k) keys[k] = key_of(turn ^ 1, k);
+      uint64_t any_gone = 0;
 #pragma unroll
-          for (int g = 0; g < RG; ++g)
-#pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) s[g][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[g][p][st], s[g][i], 0, 0, 0);
-        }
-      const uint64_t any_gone = b.gone[0] | b.gone[1] | b.gone[2] | b.gone[3];
+      for (int w = 0; w < WAVES; ++w) any_gone |= b.gone[w];
       const uint32_t gone32 = __builtin_amdgcn_readfirstlane((uint32_t)any_gone | (uint32_t)(any_gone >> 32));
       if (base < wave_all_low || base + kTile > wave_all_end || gone32) {
 #pragma unroll
@@ -187,137 +214,175 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int at = 32 * i + 8 * (e / 4) + 4 * half + e % 4, key = base + at;
-            const bool gone = b.gone[at / 16] >> (4 * (at % 16)) & 1;
-#pragma unroll
-            for (int g = 0; g < RG; ++g)
-              if (key < low[g] || key >= end[g] || gone) s[g][i][e] = -INFINITY;
+            const bool gone = b.gone[at / kKeysAWave] >> (PARTS * (at % kKeysAWave)) & 1;
+            if (key < low || key >= end || gone) s.s[i][e] = -INFINITY;
           }
+        most = most_of(s);
       }
-      // softmax: the maximum is raised only where scores are 2^kSlack times beyond it, the sums hold that
+      // the maximum is raised only where scores are 2^kSlack times beyond it: the sums hold that
       constexpr float kSlack = 6.0f;
-      at_b8 pr[RG][PIECES][4];
+      most = pair_max(most) * factor;
+      if (__ballot(most > m + kSlack)) {
+        const float raised = fmaxf(m, most), fade = raised == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - raised);
+        m = raised;
+        l *= fade;
 #pragma unroll
-      for (int g = 0; g < RG; ++g) {
-        float most = s[g][0][0];
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) most = fmaxf(most, s[g][i][e]);
-        most = pair_max(most) * factor;
-        if (__ballot(most > m[g] + kSlack)) {
-          const float raised = fmaxf(m[g], most), fade = raised == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[g] - raised);
-          m[g] = raised;
-          l[g] *= fade;
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[g][d][e] *= fade;
-        }
-        const float zero = m[g] == -INFINITY ? 0.0f : -m[g];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][i][e], factor, zero));
-            l[g] += p;
-            __bf16 piece[PIECES];
-            attention_split<PIECES>(p, piece);
-#pragma unroll
-            for (int k = 0; k < PIECES; ++k) pr[g][k][2 * i + e / 8][e % 8] = piece[k];
-          }
+          for (int e = 0; e < 16; ++e) o[d][e] *= fade;
       }
-      // O^T
+      const float zero = m == -INFINITY ? 0.0f : -m;
+      mx_u4 pr[PIECES][4];
+      const auto probability = [&](int e) {  // elements e and e + 1
+        float x[2];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+        for (int j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s.s[(e + j) / 16][(e + j) % 16], factor, zero));
+        l += x[0] + x[1];
+        __bf16 piece[2][PIECES];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          union {
-            at_s4 half[2];
-            at_b8 whole;
-          } v;
-          const int row = 16 * u + 4 * half + (lane & 15) / 4, col = 32 * d + (lane & 16) + 4 * (lane & 3);
-          v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)(b.values + row * kValueRow + 2 * col));
-          v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)(b.values + (row + 8) * kValueRow + 2 * col));
+        for (int j = 0; j < 2; ++j) attention_split<PIECES>(x[j], piece[j]);
 #pragma unroll
-          for (int g = 0; g < RG; ++g)
-#pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) o[g][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.whole, pr[g][p][u], o[g][d], 0, 0, 0);
+        for (int k = 0; k < PIECES; ++k) {
+          uint32_t pair = __builtin_bit_cast(uint32_t, at_b2{piece[0][k], piece[1][k]});
+          asm volatile("" : "+v"(pair), "+v"(l));  // here, not where it is used
+          pr[k][e / 8][e % 8 / 2] = pair;
         }
-      constexpr int kScales = ValueChunk::kScales;
+      };
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < kProducts; ++k) {
+        score(next, k, keys[k % kAhead]);
+        if (k + kAhead < kProducts) keys[k % kAhead] = key_of(turn ^ 1, k + kAhead);
+        else values[(k + kAhead) % kAhead] = value_of(turn, k + kAhead - kProducts);
+#pragma unroll
+        for (int e = 32 * k / kProducts; e < 32 * (k + 1) / kProducts; ++e)
+          if (e % 2) probability(e - 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      most = next.s[0][0];
+#pragma unroll
+      for (int k = 0; k < kProducts; ++k) {
+        const int u = k / DB, d = k % DB;
+#pragma unroll
+        for (int p = PIECES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values[k % kAhead], __builtin_bit_cast(at_b8, pr[p][u]), o[d], 0, 0, 0);
+        if (k + kAhead < kProducts) values[k % kAhead] = value_of(turn, k + kAhead);
+        if (k < kForward) forward(turn, base, k);
+        if (k == kProducts - 1)
+#pragma unroll
+          for (int f = kProducts; f < kForward; ++f) forward(turn, base, f);
+#pragma unroll
+        for (int e = 32 * k / kProducts; e < 32 * (k + 1) / kProducts; ++e) most = fmaxf(most, next.s[e / 16][e % 16]);
+        asm volatile("" : "+v"(most));
+        __builtin_amdgcn_sched_barrier(0);
+      }
       uint64_t any_none = 0;
 #pragma unroll
-      for (int x = 0; x < kScales; ++x) any_none |= b.none[x][0] | b.none[x][1] | b.none[x][2] | b.none[x][3];
+      for (int w = 0; w < WAVES * ValueChunk::kScales; ++w) any_none |= b.none[0][w];
       if (__builtin_amdgcn_readfirstlane((uint32_t)any_none | (uint32_t)(any_none >> 32))) {
-        // NaN for the queries that see such a value, and for no other: block d is part 4 d / DB, or half of it
+        // NaN for the queries that see such a value, and for no other: block d lies in part d PARTS / DB
+        constexpr int kScales = ValueChunk::kScales;
         for (int at = 0; at < kTile; ++at) {
-          const uint32_t bits0 = (uint32_t)(b.none[0][at / 16] >> (4 * (at % 16))) & 15, bits1 = kScales > 1 ? (uint32_t)(b.none[kScales - 1][at / 16] >> (4 * (at % 16))) & 15 : 0;
-          if (!(bits0 | bits1)) continue;
+          uint32_t bits[kScales], any = 0;
 #pragma unroll
-          for (int g = 0; g < RG; ++g) {
-            const bool seen = base + at >= low[g] && base + at < end[g];
+          for (int x = 0; x < kScales; ++x) {
+            bits[x] = (uint32_t)(b.none[x][at / kKeysAWave] >> (PARTS * (at % kKeysAWave))) & ((1 << PARTS) - 1);
+            any |= bits[x];
+          }
+          if (!any) continue;
+          const bool seen = base + at >= low && base + at < end;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-              const bool nan = (DB == 8 && d % 2 ? bits1 : bits0) >> (DB == 2 ? 2 * d : DB == 4 ? d : d / 2) & 1;
+          for (int d = 0; d < DB; ++d) {
+            const bool nan = bits[d % kScales] >> (d * PARTS / DB) & 1;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[g][d][e] = nan && seen ? NAN : o[g][d][e];
-            }
+            for (int e = 0; e < 16; ++e) o[d][e] = nan && seen ? NAN : o[d][e];
           }
         }
       }
-    }
-    if (base + kTile < k1) {
-      store(buffers[turn ^ 1]);
-      load(base + 2 * kTile);
-      look_up(base + 3 * kTile);
+    } else {
+      if (seen_by_wave(base + kTile)) {
+        all_scores(turn ^ 1, next);
+        most = most_of(next);
+      }
+#pragma unroll
+      for (int k = 0; k < kForward; ++k) forward(turn, base, k);
     }
     __syncthreads();
+  };
+
+  Scores even, odd;
+  if (k0 < k1) {
+    look_up(k0);
+    value_place = place_of(k0);
+    values_there = there;
+    kc.load(c.k_codes, c.k_scales, value_place, blocks, part);
+    vc.load(c.v_codes, c.v_scales, value_place, blocks, part);
+    look_up(k0 + kTile);
+    prepare_values(0, values_there);
+#pragma unroll
+    for (int st = 0; st < kChunk; ++st) store_keys(0, st), store_values(0, st);
+    value_place = place_of(k0 + kTile);
+    values_there = there;
+    kc.load(c.k_codes, c.k_scales, value_place, blocks, part);
+    vc.load(c.v_codes, c.v_scales, value_place, blocks, part);
+    look_up(k0 + 2 * kTile);
+#pragma unroll
+    for (int st = 0; st < kChunk; ++st) store_keys(1, st);
+    value_place = place_of(k0 + 2 * kTile);
+    keys_there = there;
+    kc.load(c.k_codes, c.k_scales, value_place, blocks, part);
+    look_up(k0 + 3 * kTile);
+    __syncthreads();
+    if (seen_by_wave(k0)) {
+      all_scores(0, even);
+      most = most_of(even);
+    }
+    __syncthreads();  // (the first step writes over these keys)
+    for (int base = k0; base < k1; base += 2 * kTile) {
+      step(base, 0, even, odd);
+      if (base + kTile < k1) step(base + kTile, 1, odd, even);
+    }
   }
 
-  // a lane has columns 32 d + 8 i + 4 half .. + 3 of its queries
-#pragma unroll
-  for (int g = 0; g < RG; ++g) {
-    const float sum = pair_sum(l[g]);
-    const int64_t index = (int64_t)tile * ROWS + (wave * RG + g) * 32 + (lane & 31);
-    if (index >= all_rows) continue;
-    const int64_t out_row = (span.first + index / group) * a.heads + head * group + index % group;
-    if (run.runs == 1) {
-      const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-      E* out = static_cast<E*>(a.out) + out_row * c.dim;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (32 * d + 8 * i + 4 * half + j < c.dim) out[32 * d + 8 * i + 4 * half + j] = (E)(o[g][d][4 * i + j] * inverse);
-      if (half == 0) {
-        if (a.lse) a.lse[out_row] = sum == 0.0f ? -INFINITY : (m[g] + __builtin_amdgcn_logf(sum)) * kAttentionLn2;
-        work.joins[out_row] = make_int2(0, 1);
-      }
-      continue;
-    }
-    const int64_t first = run.slot + ((int64_t)tile * c.kv_heads + head) * run.runs, slot = first + split;
-    if (slot < 0 || slot >= slots) continue;  // (only offsets that break the contract)
-    const int row = (wave * RG + g) * 32 + (lane & 31);
+  // a lane has columns 32 d + 8 i + 4 half .. + 3 of its query
+  const float sum = pair_sum(l);
+  if (!row_there) return;
+  const int64_t out_row = (int64_t)(span.first + token) * a.heads + q_head;
+  if (run.runs == 1) {
+    const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    E* out = static_cast<E*>(a.out) + out_row * c.dim;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<at_f4*>(work.partial + (slot * ROWS + row) * D + 32 * d + 8 * i + 4 * half) =
-            at_f4{o[g][d][4 * i], o[g][d][4 * i + 1], o[g][d][4 * i + 2], o[g][d][4 * i + 3]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (32 * d + 8 * i + 4 * half + j < c.dim) out[32 * d + 8 * i + 4 * half + j] = (E)(o[d][4 * i + j] * inverse);
     if (half == 0) {
-      work.stats[slot * ROWS + row] = make_float2(m[g], sum);
-      if (split == 0) work.joins[out_row] = make_int2((int)(first * ROWS + row), run.runs);
+      if (a.lse) a.lse[out_row] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kAttentionLn2;
+      work.joins[out_row] = make_int2(0, 1);
     }
+    return;
+  }
+  const int64_t first = run.slot + ((int64_t)tile * c.kv_heads + head) * run.runs, slot = first + split;
+  if (slot < 0 || slot >= slots) return;  // (only offsets that break the contract)
+  const int row = wave * 32 + (lane & 31);
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<at_f4*>(work.partial + (slot * ROWS + row) * D + 32 * d + 8 * i + 4 * half) = at_f4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+  if (half == 0) {
+    work.stats[slot * ROWS + row] = make_float2(m, sum);
+    if (split == 0) work.joins[out_row] = make_int2((int)(first * ROWS + row), run.runs);
   }
 }
 
-template <int TYPE, int KF, int VF, int DB, int RG, int WAVES>
+template <int TYPE, int KF, int VF, int DB, int WAVES>
 hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
-  constexpr int D = 32 * DB, ROWS = 32 * RG * WAVES;
-  constexpr size_t bytes = 2 * (kTile * (4 * D + 80) + 96);
+  constexpr int D = 32 * DB, ROWS = 32 * WAVES;
+  constexpr size_t bytes = 2 * (kTile * (4 * D + 80) + 24 * WAVES);
   static_assert(ROWS == attention_many_rows(DB), "partials are laid out by it");
-  auto* kernel = many_kernel<TYPE, KF, VF, DB, RG, WAVES>;
+  auto* kernel = many_kernel<TYPE, KF, VF, DB, WAVES>;
   static std::atomic<uint64_t> raised{0};
   if (const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), (int)bytes, raised); e != hipSuccess) return e;
   const int group = a.heads / c.kv_heads, share_of = kAttentionManyRuns;
@@ -327,10 +392,10 @@ hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWor
 template <int TYPE, int KF, int VF>
 hipError_t with_dim(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
   switch (attention_blocks(c.dim)) {
-    case 2: return launch<TYPE, KF, VF, 2, kManyGroups<2>, kManyWaves<2>>(c, a, work, st);
-    case 4: return launch<TYPE, KF, VF, 4, kManyGroups<4>, kManyWaves<4>>(c, a, work, st);
+    case 2: return launch<TYPE, KF, VF, 2, kManyWaves<2>>(c, a, work, st);
+    case 4: return launch<TYPE, KF, VF, 4, kManyWaves<4>>(c, a, work, st);
   }
-  return launch<TYPE, KF, VF, 8, kManyGroups<8>, kManyWaves<8>>(c, a, work, st);
+  return launch<TYPE, KF, VF, 8, kManyWaves<8>>(c, a, work, st);
 }
 template <int TYPE>
 hipError_t with_formats(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
