@@ -74,26 +74,15 @@ struct AttentionWork {
   int2* joins;      // [T][heads]: the row of the first of its partials, number of partials
 };
 
-template <int WAVES>
-__device__ __forceinline__ int64_t attention_scan(int64_t v, int64_t* totals, int64_t& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  int64_t sum = v;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t other = __shfl_up(sum, d);
-    if (lane >= d) sum += other;
-  }
-  if (lane == 63) totals[wave] = sum;
-  __syncthreads();
-  total = 0;
-  int64_t before = 0;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    if (w < wave) before += totals[w];
-    total += totals[w];
-  }
-  __syncthreads();
-  return before + sum - v;
+// Sums over the lanes up to each.
+__device__ __forceinline__ uint32_t attention_scan(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);   // row_shr:1
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);   // row_shr:2
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);   // row_shr:4
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);   // row_shr:8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);  // row_bcast:15, into the odd rows
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);  // row_bcast:31, into the last two
+  return v;
 }
 
 // A workgroup's run of keys.
@@ -101,51 +90,49 @@ struct AttentionRun {
   int seq, local, runs, slot;  // place among the sequence's runs, runs of a unit, first partial of the sequence (-1: none)
 };
 
-// Units are (ROWS rows, head); each is cut into ceil(blocks / share) runs, a block being BLOCK keys, such that there are about `share_of` of them: at most
-// that many and as many as units, and of those of units that are cut at most twice as many.
-template <int THREADS, int ROWS, int BLOCK>
-__device__ __forceinline__ bool attention_run(const CacheArgs& c, const AttentionArgs& a, int group, int share_of, int64_t id, AttentionRun& run) {
-  __shared__ int64_t totals[THREADS / 64];
-  __shared__ AttentionRun found;
-  const int tid = threadIdx.x;
-  const auto sizes = [&](int s, int64_t& units, int64_t& blocks) {
-    units = 0, blocks = 0;
+// Units are (ROWS rows, head); each is cut into ceil(blocks / share) runs, a block being BLOCK keys, such that there are about SHARES of them: at most
+// that many and as many as units, and of those of units that are cut at most twice as many.  Every wavefront finds the run for itself, 64 sequences
+// at a time.  (Offsets that break the contract can make counts wrap: what is found then is still inside its sequence.)
+template <int ROWS, int BLOCK, int SHARES>
+__device__ __forceinline__ bool attention_run(const CacheArgs& c, const AttentionArgs& a, uint32_t group, uint32_t id, AttentionRun& run) {
+  static_assert((SHARES & (SHARES - 1)) == 0);
+  const int lane = threadIdx.x & 63;
+  uint32_t units = 0, blocks = 1;
+  const auto sizes = [&](int s) {
+    units = 0, blocks = 1;
     if (s >= c.seqs) return;
     const AttentionSpan span = attention_span(c, a, s);
-    units = ((int64_t)span.rows * group + ROWS - 1) / ROWS * c.kv_heads;
-    blocks = span.high > span.low ? (span.high - (span.low & ~15) + BLOCK - 1) / BLOCK : 1;
+    units = ((uint32_t)span.rows * group + ROWS - 1) / ROWS * c.kv_heads;
+    if (span.high > span.low) blocks = (uint32_t)(span.high - (span.low & ~15) + BLOCK - 1) / BLOCK;
   };
-  int64_t units, blocks, all = 0;
-  for (int s = 0; s < c.seqs; s += THREADS) {
-    int64_t total;
-    sizes(s + tid, units, blocks);
-    attention_scan<THREADS / 64>(units * blocks, totals, total);
-    all += total;
+  uint64_t all = 0;
+  for (int s = 0; s < c.seqs; s += 64) {
+    sizes(s + lane);
+    all += (uint64_t)units * blocks;
   }
-  const int64_t share = all > share_of ? (all + share_of - 1) / share_of : 1;
-  if (tid == 0) found.seq = -1;
-  int64_t before = 0, slots_before = 0;
-  for (int s = 0; s < c.seqs; s += THREADS) {
-    if (c.seqs > THREADS) sizes(s + tid, units, blocks);
-    const int64_t runs = (blocks + share - 1) / share;
-    // (both counts below 2^31)
-    int64_t total;
-    const int64_t at = attention_scan<THREADS / 64>(units * runs << 32 | (runs > 1 ? units * runs : 0), totals, total);
-    const int64_t first = before + (at >> 32);
-    if (id >= first && id < first + units * runs)
-      found = AttentionRun{s + tid, (int)(id - first), (int)runs, runs > 1 ? (int)(slots_before + (at & 0xffffffff)) : -1};
-    before += total >> 32;
-    slots_before += total & 0xffffffff;
-    if (before > id) break;
+  if (c.seqs > 1)
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
+  const uint64_t wide = (all + SHARES - 1) / SHARES;
+  const uint32_t share = __builtin_amdgcn_readfirstlane(wide > 0x7fffffffu ? 0x7fffffffu : wide ? (uint32_t)wide : 1);
+  uint32_t before = 0, slots_before = 0;
+  for (int s = 0; s < c.seqs; s += 64) {
+    if (c.seqs > 64) sizes(s + lane);
+    const uint32_t runs = blocks > share ? (blocks + share - 1) / share : 1, count = units * runs, cut = runs > 1 ? count : 0;
+    const uint32_t upto = attention_scan(count), slots_upto = attention_scan(cut);
+    const uint64_t found = __ballot(id - before - (upto - count) < count);
+    if (found) {
+      const int at = __builtin_ctzll(found);
+      run.seq = s + at;
+      run.local = (int)(id - before - __builtin_amdgcn_readlane(upto - count, at));
+      run.runs = (int)__builtin_amdgcn_readlane(runs, at);
+      run.slot = run.runs > 1 ? (int)(slots_before + __builtin_amdgcn_readlane(slots_upto - cut, at)) : -1;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+    slots_before += __builtin_amdgcn_readlane(slots_upto, 63);
   }
-  __syncthreads();
-  run = found;
-  // (the same in all lanes, which the compiler does not know of what lies in LDS)
-  run.seq = __builtin_amdgcn_readfirstlane(run.seq);
-  run.local = __builtin_amdgcn_readfirstlane(run.local);
-  run.runs = __builtin_amdgcn_readfirstlane(run.runs);
-  run.slot = __builtin_amdgcn_readfirstlane(run.slot);
-  return run.seq >= 0;
+  return false;
 }
 
 // A lane's part of a key or value: 8 DB codes.
@@ -158,23 +145,36 @@ struct AttentionChunk {
   uint32_t w[kWords];
   uint32_t scale[kScales];
 
-  // Of any row that there is.  Where a row has fewer blocks than DB, the pieces behind its end are others of its own: queries are zero there, and
-  // results are not kept.
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t place, int blocks, int part) {
+  // Bytes from a row's first code, and block from its first, of load i.  Where a row has fewer blocks than the kernel is made for, those behind its end are
+  // others of its own: queries are zero there, and results are not kept.
+  static __device__ __forceinline__ uint32_t code_at(int blocks, int part, int i) {
+    const int at = part * kWords + i * kPiece, most = blocks * kRowWords - kPiece;
+    return 4 * (at < most ? at : most);
+  }
+  static __device__ __forceinline__ uint32_t scale_at(int blocks, int part, int i) {
+    const int block = part * DB / 4 + i;
+    return block < blocks ? block : blocks - 1;
+  }
+  static constexpr int kLoads = kWords / kPiece;
+  // codes and scales of a row (any that there is), `code` and `scale` as above
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, const uint32_t (&code)[kLoads], const uint32_t (&scale_of)[kScales]) {
     typedef uint32_t piece __attribute__((ext_vector_type(kPiece)));
-    const uint32_t* row = reinterpret_cast<const uint32_t*>(codes) + place * (blocks * kRowWords);
 #pragma unroll
-    for (int i = 0; i < kWords; i += kPiece) {
-      const int at = part * kWords + i, most = blocks * kRowWords - kPiece;
-      const piece p = *reinterpret_cast<const piece*>(row + (at < most ? at : most));
+    for (int i = 0; i < kLoads; ++i) {
+      const piece p = *reinterpret_cast<const piece*>(codes + code[i]);
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) w[i + k] = p[k];
+      for (int k = 0; k < kPiece; ++k) w[i * kPiece + k] = p[k];
     }
 #pragma unroll
-    for (int i = 0; i < kScales; ++i) {
-      const int block = part * DB / 4 + i;
-      scale[i] = scales[place * blocks + (block < blocks ? block : blocks - 1)];
-    }
+    for (int i = 0; i < kScales; ++i) scale[i] = scales[scale_of[i]];
+  }
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t place, int blocks, int part) {
+    uint32_t code[kLoads], scale_of[kScales];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) code[i] = code_at(blocks, part, i);
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) scale_of[i] = scale_at(blocks, part, i);
+    load(codes + place * (blocks * kRowWords * 4), scales + place * blocks, code, scale_of);
   }
   // eight codes of step st
   __device__ __forceinline__ at_b8 values(int st) const {
@@ -185,8 +185,11 @@ struct AttentionChunk {
 // Host side: blocks of 32 columns that the kernels are made for, and what the kernel for many rows has of rows and runs.
 constexpr int attention_blocks(int64_t dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
 template <int DB>
+constexpr int kManyGroups = 1;  // of 32 rows
+template <int DB>
 constexpr int kManyWaves = DB == 8 ? 4 : 8;
 constexpr int attention_many_rows(int db) { return 32 * (db == 2 ? kManyWaves<2> : db == 4 ? kManyWaves<4> : kManyWaves<8>); }
+constexpr int attention_many_slots(int db) { return db == 8 ? 2 : 3; }  // (two of 256 columns take 141 KB)
 constexpr int kAttentionManyRuns = 256;
 hipError_t launch_attention_many(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st);
 

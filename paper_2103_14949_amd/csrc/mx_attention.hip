@@ -32,7 +32,7 @@ __device__ __forceinline__ float sum_of_parts(float v) {
 }
 
 template <int TYPE, int KF, int VF, int DB>
-__global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void attention_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int group) {
+__global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void attention_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, uint32_t group) {
   using E = typename MxElement<TYPE>::type;
   constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB;
   constexpr int kRow = 2 * D + 32;                          // bytes of a row of values in LDS: 4 x 16 elements of it fall on different banks
@@ -42,20 +42,22 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   __shared__ __align__(16) uint8_t lds[kWaves * kRegion];
 
   AttentionRun run;
-  if (!attention_run<kThreads, kRows, kBlock>(c, a, group, kRuns<DB>, blockIdx.x, run)) return;
+  if (!attention_run<kRows, kBlock, kRuns<DB>>(c, a, group, blockIdx.x, run)) return;
   const AttentionSpan span = attention_span(c, a, run.seq);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, part = lane / 16;
-  const int tiles = (int)(((int64_t)span.rows * group + 15) / 16);
-  const int head = run.local % c.kv_heads, tile = run.local / c.kv_heads % tiles, split = run.local / c.kv_heads / tiles;
+  // (rows of all heads: at most 2^27)
+  const uint32_t all_rows = (uint32_t)span.rows * group, tiles = (all_rows + kRows - 1) / kRows;
+  const uint32_t unit = (uint32_t)run.local / (uint32_t)c.kv_heads;
+  const int head = run.local - (int)unit * c.kv_heads, split = (int)(unit / tiles), tile = (int)(unit - (uint32_t)split * tiles);
   const int blocks = (c.dim + 31) / 32;
   const float factor = a.scale * kAttentionLog2e;
 
   // this lane's query: its row of the call, and the keys it sees
-  const int64_t index = (int64_t)tile * 16 + r;
-  const bool row_there = index < (int64_t)span.rows * group;
+  const uint32_t index = (uint32_t)tile * kRows + r;
+  const bool row_there = index < all_rows;
   const int token = row_there ? (int)(index / group) : 0;
   const int64_t t = span.first + token;
-  const int q_head = head * group + (int)(index - (int64_t)token * group);
+  const int q_head = head * (int)group + (row_there ? (int)(index - token * group) : 0);
   const auto end_of = [&](int i) {
     const int64_t p = span.position + i + 1;
     return !a.causal || p > span.high ? span.high : p < 0 ? 0 : (int)p;
@@ -85,13 +87,13 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   }
 
   // the keys of this run that any of the tile's rows sees
-  const int64_t last_row = ((int64_t)tile + 1) * 16 < (int64_t)span.rows * group ? ((int64_t)tile + 1) * 16 - 1 : (int64_t)span.rows * group - 1;
+  const uint32_t first_row = (uint32_t)tile * kRows, last_row = first_row + kRows < all_rows ? first_row + kRows - 1 : all_rows - 1;
   const int start = span.low & ~15, all_blocks = span.high > span.low ? (span.high - start + kBlock - 1) / kBlock : 1;
   const int each = (all_blocks + run.runs - 1) / run.runs;
   // (positions stay 2^16 below 2^31; of the runs' ends only what is below `high` counts)
   const int64_t run_first = start + (int64_t)split * each * kBlock, run_end = run_first + (int64_t)each * kBlock;
   int k0 = run_first < span.high ? (int)run_first : span.high, k1 = run_end < span.high ? (int)run_end : span.high;
-  const int tile_low = low_of((int)((int64_t)tile * 16 / group)) & ~15, tile_end = end_of((int)(last_row / group));
+  const int tile_low = low_of((int)(first_row / group)) & ~15, tile_end = end_of((int)(last_row / group));
   if (k0 < tile_low) k0 = tile_low;
   if (k1 > tile_end) k1 = tile_end;
 
@@ -228,9 +230,9 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) y[i] = __builtin_fmaf(reinterpret_cast<const float*>(lds + w * kRegion)[row * kSums + col + i], weight[w], y[i]);
   }
-  const int64_t out_index = (int64_t)tile * 16 + row;
-  if (out_index >= (int64_t)span.rows * group) return;
-  const int64_t out_row = (span.first + out_index / group) * a.heads + head * group + out_index % group;
+  const uint32_t out_index = first_row + row;
+  if (out_index >= all_rows) return;
+  const int64_t out_row = (int64_t)(span.first + out_index / group) * a.heads + head * group + out_index % group;
   if (run.runs == 1) {
     const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
@@ -253,21 +255,33 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
 }
 
 // Joins the runs of a row, whose partials are `apart` rows apart.  Four columns a thread, the runs by turns; the order of the sums is the runs'.
+// (A workgroup for every row of a prompt of 8192, 32 heads, took XX us to find that there is nothing to join.)
 template <int TYPE, int DB>
-__global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int64_t rows, int apart, int slots) {
+__global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int64_t rows, int each, int apart, int slots) {
   using E = typename MxElement<TYPE>::type;
   constexpr int D = 32 * DB, kColumns = D / 4, kTurns = kThreads / kColumns;
   __shared__ float weights[kMostRuns];
   __shared__ float shared[kWaves][2];
   __shared__ at_f4 sums[kTurns][kColumns];
   const int tid = threadIdx.x;
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    const int64_t t = row / a.heads;
-    if (t < c.offsets[0] || t >= c.offsets[c.seqs]) continue;
-    const int2 join = work.joins[row];
-    const int runs = join.y;
+  // Which of this workgroup's rows were cut (every wavefront looks at all of them): none of a long prompt's, whose units are many
+  const int64_t first = (int64_t)blockIdx.x * each, mine = first + (tid & 63);
+  bool cut = (tid & 63) < each && mine < rows;
+  int2 whose = make_int2(0, 0);
+  if (cut) {
+    const int64_t t = mine / a.heads;
+    cut = t >= c.offsets[0] && t < c.offsets[c.seqs];
+  }
+  if (cut) {
+    whose = work.joins[mine];
     // (what no sequence wrote may be anything)
-    if (runs < 2 || runs > kMostRuns || join.x < 0 || (int64_t)join.x + (int64_t)apart * (runs - 1) >= (int64_t)apart * slots) continue;
+    cut = whose.y >= 2 && whose.y <= kMostRuns && whose.x >= 0 && (int64_t)whose.x + (int64_t)apart * (whose.y - 1) < (int64_t)apart * slots;
+  }
+  for (uint64_t left = __ballot(cut); left; left &= left - 1) {
+    const int at = __builtin_ctzll(left);
+    const int64_t row = first + at;
+    const int2 join = make_int2(__builtin_amdgcn_readlane(whose.x, at), __builtin_amdgcn_readlane(whose.y, at));
+    const int runs = join.y;
     float most = -INFINITY, sum = 0.0f;
     for (int i = tid; i < runs; i += kThreads) most = fmaxf(most, work.stats[join.x + (int64_t)apart * i].x);
 #pragma unroll
@@ -320,8 +334,9 @@ constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }
 
 template <int TYPE, int DB>
 hipError_t launch_join(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, int apart, int slots, hipStream_t st) {
-  const int64_t rows = (int64_t)a.T * a.heads, most = max_blocks(kThreads);
-  return launch_kernel(join_kernel<TYPE, DB>, dim3((uint32_t)(rows < most ? rows : most)), dim3(kThreads), 0, st, c, a, work, rows, apart, slots);
+  // a row a workgroup while there are few
+  const int64_t rows = (int64_t)a.T * a.heads, each = rows < 4096 ? 1 : rows < 64 * 4096 ? (rows + 4095) / 4096 : 64;
+  return launch_kernel(join_kernel<TYPE, DB>, dim3((uint32_t)((rows + each - 1) / each)), dim3(kThreads), 0, st, c, a, work, rows, (int)each, apart, slots);
 }
 template <int TYPE, int KF, int VF, int DB>
 hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
@@ -331,7 +346,7 @@ hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWor
     return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(DB), 2 * kAttentionManyRuns, st);
   }
   const int64_t units = ((int64_t)a.T * group / kRows + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
-  const hipError_t e = launch_kernel(attention_kernel<TYPE, KF, VF, DB>, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, group);
+  const hipError_t e = launch_kernel(attention_kernel<TYPE, KF, VF, DB>, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, (uint32_t)group);
   return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, kRows, 2 * kRuns<DB>, st);
 }
 template <int TYPE, int KF, int VF>
