@@ -254,22 +254,21 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   }
 }
 
-// Joins the runs of a row, whose partials are `apart` rows apart.  Four columns a thread, the runs by turns; the order of the sums is the runs'.
-// (A workgroup for every row of a prompt of 8192, 32 heads, took XX us to find that there is nothing to join.)
-template <int TYPE, int DB>
+// Joins the runs of a row, whose partials are `apart` rows apart: by the four wavefronts of a workgroup where there are few rows (PARTS 4; a long sequence's token has up
+// to a run a CU), by one where there are many.  The order of the sums is the runs' in either.  A wavefront looks at `each` rows together for those that were cut:
+// none of a long prompt's, whose units are many (a workgroup for every row of 8192 x 32 took 120 us to find nothing).
+template <int TYPE, int DB, int PARTS>
 __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int64_t rows, int each, int apart, int slots) {
   using E = typename MxElement<TYPE>::type;
-  constexpr int D = 32 * DB, kColumns = D / 4, kTurns = kThreads / kColumns;
-  __shared__ float weights[kMostRuns];
-  __shared__ float shared[kWaves][2];
-  __shared__ at_f4 sums[kTurns][kColumns];
-  const int tid = threadIdx.x;
-  // Which of this workgroup's rows were cut (every wavefront looks at all of them): none of a long prompt's, whose units are many
-  const int64_t first = (int64_t)blockIdx.x * each, mine = first + (tid & 63);
-  bool cut = (tid & 63) < each && mine < rows;
+  constexpr int D = 32 * DB, kColumns = D / 64;  // a lane's
+  typedef float columns __attribute__((ext_vector_type(kColumns)));
+  __shared__ columns sums[PARTS - 1 ? PARTS - 1 : 1][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), part = PARTS == 1 ? 0 : wave;
+  const int64_t first = (PARTS == 1 ? (int64_t)blockIdx.x * kWaves + wave : (int64_t)blockIdx.x) * each, mine = first + lane;
+  bool cut = lane < each && mine < rows;
   int2 whose = make_int2(0, 0);
   if (cut) {
-    const int64_t t = mine / a.heads;
+    const int t = (int)((uint32_t)mine / (uint32_t)a.heads);  // (rows of all heads: at most 2^27)
     cut = t >= c.offsets[0] && t < c.offsets[c.seqs];
   }
   if (cut) {
@@ -280,49 +279,42 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
   for (uint64_t left = __ballot(cut); left; left &= left - 1) {
     const int at = __builtin_ctzll(left);
     const int64_t row = first + at;
-    const int2 join = make_int2(__builtin_amdgcn_readlane(whose.x, at), __builtin_amdgcn_readlane(whose.y, at));
-    const int runs = join.y;
+    const int from = __builtin_amdgcn_readlane(whose.x, at), runs = __builtin_amdgcn_readlane(whose.y, at);
+    const float2* stats = work.stats + from;
     float most = -INFINITY, sum = 0.0f;
-    for (int i = tid; i < runs; i += kThreads) most = fmaxf(most, work.stats[join.x + (int64_t)apart * i].x);
+    for (int i = lane; i < runs; i += 64) most = fmaxf(most, stats[(int64_t)apart * i].x);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    __syncthreads();
-    if ((tid & 63) == 0) shared[tid / 64][0] = most;
-    __syncthreads();
-    most = fmaxf(fmaxf(shared[0][0], shared[1][0]), fmaxf(shared[2][0], shared[3][0]));
     const float zero = most == -INFINITY ? 0.0f : most;
-    for (int i = tid; i < runs; i += kThreads) {
-      const float2 s = work.stats[join.x + (int64_t)apart * i];
-      const float w = __builtin_amdgcn_exp2f(s.x - zero);
-      weights[i] = w;
-      sum = __builtin_fmaf(s.y, w, sum);
+    for (int i = lane; i < runs; i += 64) {
+      const float2 s = stats[(int64_t)apart * i];
+      sum = __builtin_fmaf(s.y, __builtin_amdgcn_exp2f(s.x - zero), sum);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    if ((tid & 63) == 0) shared[tid / 64][1] = sum;
-    __syncthreads();
-    sum = (shared[0][1] + shared[1][1]) + (shared[2][1] + shared[3][1]);
-    const int col = tid % kColumns, turn = tid / kColumns;
-    at_f4 y = {};
-    for (int i = turn; i < runs; i += kTurns) {
-      const at_f4 p = *reinterpret_cast<const at_f4*>(work.partial + (join.x + (int64_t)apart * i) * D + 4 * col);
+    columns y = {};
+    const float* partial = work.partial + (int64_t)from * D + lane * kColumns;
+#pragma unroll 4
+    for (int i = part; i < runs; i += PARTS) {
+      const float w = __builtin_amdgcn_exp2f(stats[(int64_t)apart * i].x - zero);
+      const columns p = *reinterpret_cast<const columns*>(partial + (int64_t)apart * i * D);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = __builtin_fmaf(p[k], weights[i], y[k]);
+      for (int k = 0; k < kColumns; ++k) y[k] = __builtin_fmaf(p[k], w, y[k]);
     }
-    sums[turn][col] = y;
-    __syncthreads();
-    if (turn == 0) {
+    if constexpr (PARTS > 1) {
+      if (part) sums[part - 1][lane] = y;
+      __syncthreads();  // (all wavefronts go through the same rows)
+      if (part) continue;
 #pragma unroll
-      for (int i = 1; i < kTurns; ++i)
+      for (int i = 0; i < PARTS - 1; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] += sums[i][col][k];
-      const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (4 * col + k < c.dim) static_cast<E*>(a.out)[row * c.dim + 4 * col + k] = (E)(y[k] * inverse);
-      if (a.lse && col == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kAttentionLn2;
+        for (int k = 0; k < kColumns; ++k) y[k] += sums[i][lane][k];
     }
-    __syncthreads();
+    const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int k = 0; k < kColumns; ++k)
+      if (kColumns * lane + k < c.dim) static_cast<E*>(a.out)[row * c.dim + kColumns * lane + k] = (E)(y[k] * inverse);
+    if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kAttentionLn2;
   }
 }
 
@@ -334,9 +326,11 @@ constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }
 
 template <int TYPE, int DB>
 hipError_t launch_join(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, int apart, int slots, hipStream_t st) {
-  // a row a workgroup while there are few
-  const int64_t rows = (int64_t)a.T * a.heads, each = rows < 4096 ? 1 : rows < 64 * 4096 ? (rows + 4095) / 4096 : 64;
-  return launch_kernel(join_kernel<TYPE, DB>, dim3((uint32_t)((rows + each - 1) / each)), dim3(kThreads), 0, st, c, a, work, rows, (int)each, apart, slots);
+  const int64_t rows = (int64_t)a.T * a.heads;
+  if (rows <= 4096)  // a row a workgroup
+    return launch_kernel(join_kernel<TYPE, DB, 4>, dim3((uint32_t)rows), dim3(kThreads), 0, st, c, a, work, rows, 1, apart, slots);
+  const int64_t each = rows < 64 * 8192 ? (rows + 8191) / 8192 : 64, waves = (rows + each - 1) / each;
+  return launch_kernel(join_kernel<TYPE, DB, 1>, dim3((uint32_t)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, c, a, work, rows, (int)each, apart, slots);
 }
 template <int TYPE, int KF, int VF, int DB>
 hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {

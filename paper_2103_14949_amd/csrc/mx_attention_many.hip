@@ -79,25 +79,38 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   at_b8 q[PIECES][STEPS];
   const uint32_t index = (uint32_t)tile * ROWS + wave * 32 + (lane & 31);
   const bool row_there = index < all_rows;
-  const int token = row_there ? (int)(index / group) : 0;
+  const int token = row_there ? (int)(index / group) : 0;  // (the first row where there is none)
   const int q_head = head * (int)group + (row_there ? (int)(index - token * group) : 0);
   const int low = row_there ? low_of(token) : 0, end = row_there ? end_of(token) : 0;
+  {
+    typedef E elements __attribute__((ext_vector_type(8)));
+    typedef elements elements_any __attribute__((aligned(sizeof(E))));
+    const E* const row = static_cast<const E*>(a.q.data) + (int64_t)(span.first + token) * a.q.row + (int64_t)q_head * a.q.head;
+    elements x[STEPS] = {};
+    if (c.dim % 8 == 0) {
+      // all under way before the first is waited for; columns behind the last are others of the row, and zero after that
 #pragma unroll
-  for (int st = 0; st < STEPS; ++st) {
-    const int col = 16 * st + 8 * half;
-    float x[8];
-    if (row_there && col < c.dim)
-      mx_load8<TYPE>(static_cast<const E*>(a.q.data) + (int64_t)(span.first + token) * a.q.row + (int64_t)q_head * a.q.head + col, c.dim - col, x);
-    else
+      for (int st = 0; st < STEPS; ++st) {
+        const int col = 16 * st + 8 * half;
+        x[st] = *reinterpret_cast<const elements_any*>(row + (col < c.dim ? col : 0));
+      }
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+      for (int st = 0; st < STEPS; ++st)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __bf16 p[PIECES];
-      attention_split<PIECES>(a.scale < 0 ? -x[i] : x[i], p);
-#pragma unroll
-      for (int k = 0; k < PIECES; ++k) q[k][st][i] = p[k];
+        for (int i = 0; i < 8; ++i)
+          if (16 * st + 8 * half + i < c.dim) x[st][i] = row[16 * st + 8 * half + i];
     }
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = row_there && 16 * st + 8 * half < c.dim ? (float)x[st][i] : 0.0f;
+        __bf16 p[PIECES];
+        attention_split<PIECES>(a.scale < 0 ? -v : v, p);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) q[k][st][i] = p[k];
+      }
   }
 
   // the keys of this run that any row of the workgroup sees, of a wavefront, and that all of its rows see
@@ -444,13 +457,24 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   if (run.runs == 1) {
     const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     E* out = static_cast<E*>(a.out) + out_row * c.dim;
+    typedef E elements __attribute__((ext_vector_type(4)));
+    typedef elements elements_any __attribute__((aligned(sizeof(E))));
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) {
+        const int col = 32 * d + 8 * i + 4 * half;
+        elements y;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (32 * d + 8 * i + 4 * half + j < c.dim) out[32 * d + 8 * i + 4 * half + j] = (E)(o[d][4 * i + j] * inverse);
+        for (int j = 0; j < 4; ++j) y[j] = (E)(o[d][4 * i + j] * inverse);
+        if (col + 4 <= c.dim) {
+          *reinterpret_cast<elements_any*>(out + col) = y;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (col + j < c.dim) out[col + j] = y[j];
+        }
+      }
     if (half == 0) {
       if (a.lse) a.lse[out_row] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kAttentionLn2;
       work.joins[out_row] = make_int2(0, 1);
