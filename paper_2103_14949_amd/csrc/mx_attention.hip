@@ -19,8 +19,8 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kRows = 16, kKeys = 32, kBlock = kWaves * kKeys;
 // Workgroups that share the keys, by blocks of a row: as many as are resident.
 template <int DB>
-constexpr int kRuns = DB == 8 ? 512 : 1024;
-constexpr int kMostRuns = 1024;
+constexpr int kRuns = DB == 8 ? 1024 : 2048;
+constexpr int kMostRuns = 2048;
 
 __device__ __forceinline__ float max_of_parts(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
@@ -31,7 +31,7 @@ __device__ __forceinline__ float sum_of_parts(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-template <int TYPE, int KF, int VF, int DB>
+template <int TYPE, int KF, int VF, int DB, bool EVEN>
 __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void attention_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, uint32_t group) {
   using E = typename MxElement<TYPE>::type;
   constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB;
@@ -67,22 +67,24 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
     return p < 0 ? 0 : p < span.high ? (int)p : span.high;
   };
   const int end = row_there ? end_of(token) : 0, low = row_there ? low_of(token) : 0;
-  at_b8 q[PIECES][DB];
+  typedef E elements __attribute__((ext_vector_type(8)));
+  typedef elements elements_any __attribute__((aligned(sizeof(E))));
+  elements x_q[DB] = {};
+  {
+    const E* const row = static_cast<const E*>(a.q.data) + t * a.q.row + (int64_t)q_head * a.q.head;
+    if (c.dim % 8 == 0) {
+      // all under way before the first is waited for; columns behind the last are others of the row, and zero after that
 #pragma unroll
-  for (int st = 0; st < DB; ++st) {
-    const int col = part * 8 * DB + 8 * st;
-    float x[8];
-    if (row_there && col < c.dim)
-      mx_load8<TYPE>(static_cast<const E*>(a.q.data) + t * a.q.row + (int64_t)q_head * a.q.head + col, c.dim - col, x);
-    else
+      for (int st = 0; st < DB; ++st) {
+        const int col = part * 8 * DB + 8 * st;
+        x_q[st] = *reinterpret_cast<const elements_any*>(row + (col < c.dim ? col : 0));
+      }
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+      for (int st = 0; st < DB; ++st)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __bf16 p[PIECES];
-      attention_split<PIECES>(x[i], p);
-#pragma unroll
-      for (int k = 0; k < PIECES; ++k) q[k][st][i] = p[k];
+        for (int i = 0; i < 8; ++i)
+          if (part * 8 * DB + 8 * st + i < c.dim) x_q[st][i] = row[part * 8 * DB + 8 * st + i];
     }
   }
 
@@ -100,27 +102,68 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   uint8_t* mine = lds + wave * kRegion;
   float m = -INFINITY, l = 0.0f;
   at_f4 o[2 * DB] = {};
-  AttentionChunk<KF, DB> kc[2];
-  AttentionChunk<VF, DB> vc[2];
-  bool there[2];  // the key has a place
+  using KeyChunk = AttentionChunk<KF, DB>;
+  using ValueChunk = AttentionChunk<VF, DB>;
+  // On their way: the pages of the keys after the next ones, the next keys and values.  Where pages are whole sixteens (EVEN), all about a tile's page is the same in
+  // every lane.
+  uint32_t key_code[KeyChunk::kLoads], value_code[ValueChunk::kLoads], key_scale[KeyChunk::kScales], value_scale[ValueChunk::kScales];
+#pragma unroll
+  for (int i = 0; i < KeyChunk::kLoads; ++i) key_code[i] = KeyChunk::code_at(blocks, part, i) + (EVEN ? r * (blocks * KeyChunk::kRowWords * 4) : 0);
+#pragma unroll
+  for (int i = 0; i < ValueChunk::kLoads; ++i) value_code[i] = ValueChunk::code_at(blocks, part, i) + (EVEN ? r * (blocks * ValueChunk::kRowWords * 4) : 0);
+#pragma unroll
+  for (int i = 0; i < KeyChunk::kScales; ++i) key_scale[i] = KeyChunk::scale_at(blocks, part, i) + (EVEN ? r * blocks : 0);
+#pragma unroll
+  for (int i = 0; i < ValueChunk::kScales; ++i) value_scale[i] = ValueChunk::scale_at(blocks, part, i) + (EVEN ? r * blocks : 0);
+  const int32_t* const table = c.table + run.seq * c.table_stride;
+  int own = 0;  // (zero; vector loads come back in the order that they are asked for)
+  asm volatile("" : "+v"(own));
+  KeyChunk kc[2];
+  ValueChunk vc[2];
+  int32_t next_page[2];
+  bool there[2];  // the page is there
+  const auto look_up = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int key = base + 16 * i + (EVEN ? 0 : r);
+      next_page[i] = -1;
+      if (key < k1) next_page[i] = table[cache_page_of(c, (uint32_t)key) + own];
+    }
+  };
   const auto load = [&](int base) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int key = base + 16 * i + r;
-      int64_t place = key < k1 ? cache_place(c, run.seq, key, head) : -1;
-      there[i] = place >= 0;
-      if (place < 0) place = 0;
-      kc[i].load(c.k_codes, c.k_scales, place, blocks, part);
-      vc[i].load(c.v_codes, c.v_scales, place, blocks, part);
+      const uint32_t key = base + 16 * i + (EVEN ? 0 : r);
+      const int32_t page = EVEN ? __builtin_amdgcn_readfirstlane(next_page[i]) : next_page[i];
+      there[i] = (uint32_t)page < (uint32_t)c.pages;
+      // (any row, where there is none)
+      const int64_t place = there[i] ? ((int64_t)page * c.kv_heads + head) * c.page + (key - cache_page_of(c, key) * (uint32_t)c.page) : 0;
+      kc[i].load(c.k_codes + place * (blocks * KeyChunk::kRowWords * 4), c.k_scales + place * blocks, key_code, key_scale);
+      vc[i].load(c.v_codes + place * (blocks * ValueChunk::kRowWords * 4), c.v_scales + place * blocks, value_code, value_scale);
     }
   };
   int base = k0 + wave * kKeys;
+  look_up(base);
   if (base < k1) load(base);
+  look_up(base + kBlock);
+  at_b8 q[PIECES][DB];
+#pragma unroll
+  for (int st = 0; st < DB; ++st)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = row_there && part * 8 * DB + 8 * st < c.dim ? (float)x_q[st][i] : 0.0f;
+      __bf16 p[PIECES];
+      attention_split<PIECES>(v, p);
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) q[k][st][i] = p[k];
+    }
   for (; base < k1; base += kBlock) {
     // S^T, values into LDS
+    constexpr int kScales = ValueChunk::kScales, kEach = ValueChunk::kWords / kScales;
     at_f4 s[2] = {};
-    uint64_t none[2][AttentionChunk<VF, DB>::kScales];  // lanes whose blocks of a value stand for NaN
-    uint32_t seen = ((uint32_t)__ballot(there[0]) & 0xffff) | (uint32_t)__ballot(there[1]) << 16;
+    uint64_t none[2][kScales] = {}, any = 0;  // lanes whose blocks of a value stand for NaN
+    uint32_t seen = EVEN ? (there[0] ? 0xffffu : 0) | (there[1] ? 0xffff0000u : 0) : ((uint32_t)__ballot(there[0]) & 0xffff) | (uint32_t)__ballot(there[1]) << 16;
+    if (k1 - base < 32) seen &= ~(~0u << (k1 - base));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -129,21 +172,28 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
 #pragma unroll
         for (int p = PIECES - 1; p >= 0; --p) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[p][st], s[i], 0, 0, 0);
       }
-      // (what has no place, and what is NaN, is zero here: a probability of zero does not take a NaN away)
-      constexpr int kScales = AttentionChunk<VF, DB>::kScales, kEach = AttentionChunk<VF, DB>::kWords / kScales;
+      bool special = false;
 #pragma unroll
-      for (int b = 0; b < kScales; ++b) {
-        const bool nan = vc[i].scale[b] == 255, zero = nan || !there[i];
-        none[i][b] = __ballot(nan && there[i]);
-        if (zero) vc[i].scale[b] = 0;
+      for (int b = 0; b < kScales; ++b) special |= vc[i].scale[b] == 255;
+      if (__ballot(special) || (seen >> (16 * i) & 0xffff) != 0xffff) {
+        // what has no place, and what is NaN, is zero in the products: a probability of zero does not take a NaN away
+        const bool mine_there = seen >> (16 * i + r) & 1;
 #pragma unroll
-        for (int w = 0; w < kEach; ++w) vc[i].w[b * kEach + w] = zero ? 0 : vc[i].w[b * kEach + w];
+        for (int b = 0; b < kScales; ++b) {
+          const bool nan = vc[i].scale[b] == 255, zero = nan || !mine_there;
+          none[i][b] = __ballot(nan && mine_there);
+          any |= none[i][b];
+          if (zero) vc[i].scale[b] = 0;
+#pragma unroll
+          for (int w = 0; w < kEach; ++w) vc[i].w[b * kEach + w] = zero ? 0 : vc[i].w[b * kEach + w];
+        }
       }
 #pragma unroll
       for (int st = 0; st < DB; ++st) *reinterpret_cast<at_b8*>(mine + (16 * i + r) * kRow + part * 16 * DB + 16 * st) = vc[i].values(st);
     }
     // the next keys and values on their way
     if (base + kBlock < k1) load(base + kBlock);
+    look_up(base + 2 * kBlock);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     // softmax: this lane's are keys base + 16 i + 4 part + j of query r
     const int from = low - base, to = end - base;
@@ -188,9 +238,6 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
 #pragma unroll
       for (int p = PIECES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.whole, pr[p], o[d], 0, 0, 0);
     }
-    uint64_t any = 0;
-#pragma unroll
-    for (int b = 0; b < AttentionChunk<VF, DB>::kScales; ++b) any |= none[0][b] | none[1][b];
     if (any) {
       // NaN for the queries that see such a value, and for no other: tile d is columns 16 d on, which part 2 d / DB holds
 #pragma unroll
@@ -340,7 +387,8 @@ hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWor
     return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(DB), 2 * kAttentionManyRuns, st);
   }
   const int64_t units = ((int64_t)a.T * group / kRows + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
-  const hipError_t e = launch_kernel(attention_kernel<TYPE, KF, VF, DB>, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, (uint32_t)group);
+  auto* kernel = c.page % 16 == 0 ? attention_kernel<TYPE, KF, VF, DB, true> : attention_kernel<TYPE, KF, VF, DB, false>;
+  const hipError_t e = launch_kernel(kernel, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, (uint32_t)group);
   return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, kRows, 2 * kRuns<DB>, st);
 }
 template <int TYPE, int KF, int VF>
