@@ -156,7 +156,9 @@ struct AttentionChunk {
     return block < blocks ? block : blocks - 1;
   }
   static constexpr int kLoads = kWords / kPiece;
-  // codes and scales of a row (any that there is), `code` and `scale` as above
+  // codes and scales of a row (any that there is), `code` and `scale_of` as above.  WORDS: scale_of are those of the words that the scales lie in; each is one only
+  // after `unpack` with its place there.  (A byte of a loop's next round is extended, and waited for, where it is loaded.)
+  template <bool WORDS>
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, const uint32_t (&code)[kLoads], const uint32_t (&scale_of)[kScales]) {
     typedef uint32_t piece __attribute__((ext_vector_type(kPiece)));
 #pragma unroll
@@ -166,15 +168,11 @@ struct AttentionChunk {
       for (int k = 0; k < kPiece; ++k) w[i * kPiece + k] = p[k];
     }
 #pragma unroll
-    for (int i = 0; i < kScales; ++i) scale[i] = scales[scale_of[i]];
+    for (int i = 0; i < kScales; ++i) scale[i] = WORDS ? *reinterpret_cast<const uint32_t*>(scales + scale_of[i]) : scales[scale_of[i]];
   }
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t place, int blocks, int part) {
-    uint32_t code[kLoads], scale_of[kScales];
+  __device__ __forceinline__ void unpack(const uint32_t (&shift)[kScales]) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) code[i] = code_at(blocks, part, i);
-#pragma unroll
-    for (int i = 0; i < kScales; ++i) scale_of[i] = scale_at(blocks, part, i);
-    load(codes + place * (blocks * kRowWords * 4), scales + place * blocks, code, scale_of);
+    for (int i = 0; i < kScales; ++i) scale[i] = scale[i] >> shift[i] & 255;
   }
   // eight codes of step st
   __device__ __forceinline__ at_b8 values(int st) const {
@@ -191,6 +189,8 @@ constexpr int kManyWaves = DB == 8 ? 4 : 8;
 constexpr int attention_many_rows(int db) { return 32 * (db == 2 ? kManyWaves<2> : db == 4 ? kManyWaves<4> : kManyWaves<8>); }
 constexpr int attention_many_slots(int db) { return db == 8 ? 2 : 3; }  // (two of 256 columns take 141 KB)
 constexpr int kAttentionManyRuns = 256;
+// Whether a wavefront's `keys` neighbours, the first at a multiple of their number, lie in one page, and their scales in words of 32 bits that are the cache's.
+inline bool attention_even(const CacheArgs& c, int keys) { return c.page % keys == 0 && ptr_aligned(c.k_scales, 4) && ptr_aligned(c.v_scales, 4); }
 hipError_t launch_attention_many(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st);
 
 constexpr float kAttentionLog2e = 1.44269504f, kAttentionLn2 = 0.693147181f;

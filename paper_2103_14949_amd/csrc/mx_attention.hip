@@ -111,10 +111,20 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   for (int i = 0; i < KeyChunk::kLoads; ++i) key_code[i] = KeyChunk::code_at(blocks, part, i) + (EVEN ? r * (blocks * KeyChunk::kRowWords * 4) : 0);
 #pragma unroll
   for (int i = 0; i < ValueChunk::kLoads; ++i) value_code[i] = ValueChunk::code_at(blocks, part, i) + (EVEN ? r * (blocks * ValueChunk::kRowWords * 4) : 0);
+  // (a tile's first place is a multiple of its keys: the scales' places in their words are a lane's own)
+  uint32_t key_shift[KeyChunk::kScales], value_shift[ValueChunk::kScales];
 #pragma unroll
-  for (int i = 0; i < KeyChunk::kScales; ++i) key_scale[i] = KeyChunk::scale_at(blocks, part, i) + (EVEN ? r * blocks : 0);
+  for (int i = 0; i < KeyChunk::kScales; ++i) {
+    const uint32_t at = KeyChunk::scale_at(blocks, part, i) + (EVEN ? r * blocks : 0);
+    key_scale[i] = EVEN ? at & ~3u : at;
+    key_shift[i] = EVEN ? (at & 3) * 8 : 0;
+  }
 #pragma unroll
-  for (int i = 0; i < ValueChunk::kScales; ++i) value_scale[i] = ValueChunk::scale_at(blocks, part, i) + (EVEN ? r * blocks : 0);
+  for (int i = 0; i < ValueChunk::kScales; ++i) {
+    const uint32_t at = ValueChunk::scale_at(blocks, part, i) + (EVEN ? r * blocks : 0);
+    value_scale[i] = EVEN ? at & ~3u : at;
+    value_shift[i] = EVEN ? (at & 3) * 8 : 0;
+  }
   const int32_t* const table = c.table + run.seq * c.table_stride;
   int own = 0;  // (zero; vector loads come back in the order that they are asked for)
   asm volatile("" : "+v"(own));
@@ -138,8 +148,8 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
       there[i] = (uint32_t)page < (uint32_t)c.pages;
       // (any row, where there is none)
       const int64_t place = there[i] ? ((int64_t)page * c.kv_heads + head) * c.page + (key - cache_page_of(c, key) * (uint32_t)c.page) : 0;
-      kc[i].load(c.k_codes + place * (blocks * KeyChunk::kRowWords * 4), c.k_scales + place * blocks, key_code, key_scale);
-      vc[i].load(c.v_codes + place * (blocks * ValueChunk::kRowWords * 4), c.v_scales + place * blocks, value_code, value_scale);
+      kc[i].template load<EVEN>(c.k_codes + place * (blocks * KeyChunk::kRowWords * 4), c.k_scales + place * blocks, key_code, key_scale);
+      vc[i].template load<EVEN>(c.v_codes + place * (blocks * ValueChunk::kRowWords * 4), c.v_scales + place * blocks, value_code, value_scale);
     }
   };
   int base = k0 + wave * kKeys;
@@ -166,6 +176,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
     if (k1 - base < 32) seen &= ~(~0u << (k1 - base));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      if (EVEN) kc[i].unpack(key_shift), vc[i].unpack(value_shift);
 #pragma unroll
       for (int st = 0; st < DB; ++st) {
         const at_b8 k = kc[i].values(st);
@@ -387,7 +398,7 @@ hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWor
     return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(DB), 2 * kAttentionManyRuns, st);
   }
   const int64_t units = ((int64_t)a.T * group / kRows + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
-  auto* kernel = c.page % 16 == 0 ? attention_kernel<TYPE, KF, VF, DB, true> : attention_kernel<TYPE, KF, VF, DB, false>;
+  auto* kernel = attention_even(c, 16) ? attention_kernel<TYPE, KF, VF, DB, true> : attention_kernel<TYPE, KF, VF, DB, false>;
   const hipError_t e = launch_kernel(kernel, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, (uint32_t)group);
   return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, kRows, 2 * kRuns<DB>, st);
 }

@@ -136,10 +136,20 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   for (int i = 0; i < KeyChunk::kLoads; ++i) key_code[i] = KeyChunk::code_at(blocks, part, i) + (EVEN ? lane / PARTS * (blocks * KeyChunk::kRowWords * 4) : 0);
 #pragma unroll
   for (int i = 0; i < ValueChunk::kLoads; ++i) value_code[i] = ValueChunk::code_at(blocks, part, i) + (EVEN ? lane / PARTS * (blocks * ValueChunk::kRowWords * 4) : 0);
+  // (a tile's first place is a multiple of its keys: the scales' places in their words are a lane's own)
+  uint32_t key_shift[KeyChunk::kScales], value_shift[ValueChunk::kScales];
 #pragma unroll
-  for (int i = 0; i < KeyChunk::kScales; ++i) key_scale[i] = KeyChunk::scale_at(blocks, part, i) + (EVEN ? lane / PARTS * blocks : 0);
+  for (int i = 0; i < KeyChunk::kScales; ++i) {
+    const uint32_t at = KeyChunk::scale_at(blocks, part, i) + (EVEN ? lane / PARTS * blocks : 0);
+    key_scale[i] = EVEN ? at & ~3u : at;
+    key_shift[i] = EVEN ? (at & 3) * 8 : 0;
+  }
 #pragma unroll
-  for (int i = 0; i < ValueChunk::kScales; ++i) value_scale[i] = ValueChunk::scale_at(blocks, part, i) + (EVEN ? lane / PARTS * blocks : 0);
+  for (int i = 0; i < ValueChunk::kScales; ++i) {
+    const uint32_t at = ValueChunk::scale_at(blocks, part, i) + (EVEN ? lane / PARTS * blocks : 0);
+    value_scale[i] = EVEN ? at & ~3u : at;
+    value_shift[i] = EVEN ? (at & 3) * 8 : 0;
+  }
   const int first_key = EVEN ? wave * kKeysAWave : loader_key;
   const int32_t* const table = c.table + run.seq * c.table_stride;
   int own = 0;  // (zero; a vector load waits for no LDS)
@@ -160,27 +170,23 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
     return there ? ((int64_t)page * c.kv_heads + head) * c.page + (key - cache_page_of(c, key) * (uint32_t)c.page) : 0;
   };
   const auto load_keys = [&](int64_t place) {
-    kc.load(c.k_codes + place * (blocks * KeyChunk::kRowWords * 4), c.k_scales + place * blocks, key_code, key_scale);
+    kc.template load<EVEN>(c.k_codes + place * (blocks * KeyChunk::kRowWords * 4), c.k_scales + place * blocks, key_code, key_scale);
   };
   const auto load_values = [&](int64_t place) {
-    vc.load(c.v_codes + place * (blocks * ValueChunk::kRowWords * 4), c.v_scales + place * blocks, value_code, value_scale);
+    vc.template load<EVEN>(c.v_codes + place * (blocks * ValueChunk::kRowWords * 4), c.v_scales + place * blocks, value_code, value_scale);
   };
   const auto store_keys = [&](int turn, int st) {
-    if (st == 0)
-#pragma unroll
-      for (int i = 0; i < KeyChunk::kScales; ++i) asm volatile("" : "+v"(kc.scale[i]));  // (32 bits, as in front of the loop)
+    if (EVEN && st == 0) kc.unpack(key_shift);
     *reinterpret_cast<at_b8*>(shared.keys[turn] + loader_key * kKeyRow + part * 16 * kChunk + 16 * st) = kc.values(st);
   };
   // Values of a tile before they go to LDS.  What has no place, and what is NaN, is zero there: a probability of zero does not take a NaN away
   const auto prepare_values = [&](int turn, int base, bool page_there) {
     Values& v = shared.values[turn];
     constexpr int kScales = ValueChunk::kScales;
+    if (EVEN) vc.unpack(value_shift);
     bool none = false;
 #pragma unroll
-    for (int s = 0; s < kScales; ++s) {
-      asm volatile("" : "+v"(vc.scale[s]));  // (32 bits, as in front of the loop)
-      none |= vc.scale[s] == 255;
-    }
+    for (int s = 0; s < kScales; ++s) none |= vc.scale[s] == 255;
     const bool there = page_there && base + loader_key < k1;
     const uint64_t gone = __ballot(!there), any_none = __ballot(none && there);
     if (lane == 0) v.flags[wave] = (gone != 0) | (any_none != 0) << 1;
@@ -249,9 +255,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   };
   const auto load_next = [&](int base) {
     values_there = keys_there;
-    if (values_there) load_values(next_place);
+    load_values(next_place);
     next_place = place_of(base + 3 * kTile, keys_there);
-    if (keys_there) load_keys(next_place);
+    load_keys(next_place);
     look_up(base + 4 * kTile);
   };
   // Tile `base`, whose scores and their largest are there: its share of the results; and the scores of the next one.  In the order that it is written in
@@ -433,11 +439,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
     }
     kc = last;
     vc = second;
-    // (the loop's scales are 32 bits wide from the start: as bytes, they would be extended, and waited for, where they are loaded)
-#pragma unroll
-    for (int i = 0; i < KeyChunk::kScales; ++i) asm volatile("" : "+v"(kc.scale[i]));
-#pragma unroll
-    for (int i = 0; i < ValueChunk::kScales; ++i) asm volatile("" : "+v"(vc.scale[i]));
     __syncthreads();
     if (seen_by_wave(k0)) {
       all_scores(0, even);
@@ -510,7 +511,7 @@ hipError_t launch_even(const CacheArgs& c, const AttentionArgs& a, const Attenti
 template <int TYPE, int KF, int VF, int DB, int WAVES>
 hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
   constexpr int keys_a_wave = kTile / WAVES;
-  return c.page % keys_a_wave == 0 ? launch_even<TYPE, KF, VF, DB, WAVES, true>(c, a, work, st) : launch_even<TYPE, KF, VF, DB, WAVES, false>(c, a, work, st);
+  return attention_even(c, keys_a_wave) ? launch_even<TYPE, KF, VF, DB, WAVES, true>(c, a, work, st) : launch_even<TYPE, KF, VF, DB, WAVES, false>(c, a, work, st);
 }
 template <int TYPE, int KF, int VF>
 hipError_t with_dim(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
