@@ -40,20 +40,48 @@ __device__ __forceinline__ void cos_sin_turns(double t, float& c, float& s) {
   if (k >= 2) s = -s;
 }
 
-// Units of eight pairs (16 columns); behind them, units of 16 columns that stay as they are.
+// i / d for i < 2^31: i * factor >> (31 + shift).
+struct Divisor {
+  uint32_t d, factor;
+  int shift;
+  explicit Divisor(uint32_t n) : d(n), factor(0), shift(0) {
+    while ((1ll << shift) < n) ++shift;
+    factor = (uint32_t)((1ull << (31 + shift)) / n + 1);
+  }
+  __device__ __forceinline__ uint32_t divide(uint32_t i) const { return (uint32_t)((uint64_t)i * factor >> (31 + shift)); }
+};
+
+// Units of eight pairs (16 columns).  Neighbours: the columns behind the last pair are in such units too, and pass; halves: they have units of their own.  Loads
+// reach to the end of a row where they may, which is eight columns at once.  A thread's next unit is under way while it turns one, its
+// first while the angles are worked out.
 template <int TYPE, bool INTERLEAVED>
-__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs r, int tokens, int heads_each, int head_groups, int64_t tiles) {
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs r, int tokens, Divisor heads_each, Divisor units, uint32_t head_groups, int64_t tiles) {
   using T = typename MxElement<TYPE>::type;
   __shared__ __align__(16) float cosines[kRopeAngles];
   __shared__ __align__(16) float sines[kRopeAngles];
-  const int pairs = r.pairs, padded = (pairs + 7) & ~7;
-  const int turned = padded / 8, rest = r.dim - 2 * pairs;
-  const bool in_place = r.out == r.x.data;
-  const int units = turned + (in_place ? 0 : (rest + 15) / 16);
+  const int pairs = r.pairs, padded = (pairs + 7) & ~7, turned = padded / 8;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int64_t t0 = tile / head_groups * tokens;
-    const int h0 = (int)(tile % head_groups) * heads_each;
-    const int nt = r.T - t0 < tokens ? (int)(r.T - t0) : tokens, nh = r.heads - h0 < heads_each ? r.heads - h0 : heads_each;
+    const int64_t unit_tile = tile / head_groups, t0 = unit_tile * tokens;
+    const int h0 = (int)(tile - unit_tile * head_groups) * (int)heads_each.d;
+    const int nt = r.T - t0 < tokens ? (int)(r.T - t0) : tokens;
+    const uint32_t all = nt * heads_each.d * units.d;
+    float a[8], b[8];
+    // unit i: its part of a row, and the row (heads behind the last: none)
+    const auto place = [&](uint32_t i, int& u, int& t, int& h) {
+      const uint32_t th = units.divide(i);
+      t = (int)heads_each.divide(th);
+      u = (int)(i - th * units.d), h = h0 + (int)(th - t * heads_each.d);
+      return i < all && h < r.heads;
+    };
+    const auto load = [&](uint32_t i) {
+      int u, t, h;
+      if (!place(i, u, t, h)) return;
+      const T* x = static_cast<const T*>(r.x.data) + (t0 + t) * r.x.row + (int64_t)h * r.x.head;
+      const int j = u * 8, first = INTERLEAVED ? 2 * j : u < turned ? j : 2 * pairs + 16 * (u - turned), second = !INTERLEAVED && u < turned ? pairs + j : first + 8;
+      mx_load8<TYPE>(x + first, r.dim - first, a);
+      if (second < r.dim) mx_load8<TYPE>(x + second, r.dim - second, b);
+    };
+    load(threadIdx.x);
     if (tile != blockIdx.x) __syncthreads();
     for (int i = threadIdx.x; i < nt * padded; i += kThreads) {
       const int t = i / padded, j = i - t * padded;
@@ -67,47 +95,47 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs r, int tokens, 
       sines[i] = s;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < nt * nh * units; i += kThreads) {
-      const int u = i % units, th = i / units, h = th % nh, t = th / nh;
-      const T* x = static_cast<const T*>(r.x.data) + (t0 + t) * r.x.row + (int64_t)(h0 + h) * r.x.head;
-      T* y = static_cast<T*>(r.out) + (t0 + t) * r.out_row + (int64_t)(h0 + h) * r.out_head;
-      float a[8], b[8];
-      if (u >= turned) {
-        const int col = 2 * pairs + (u - turned) * 16, n = r.dim - col;
-        mx_load8<TYPE>(x + col, n, a);
-        if (n > 8) mx_load8<TYPE>(x + col + 8, n - 8, b);
-        mx_store8<TYPE>(y + col, n, a);
-        if (n > 8) mx_store8<TYPE>(y + col + 8, n - 8, b);
-        continue;
-      }
+    for (uint32_t i = threadIdx.x; i < all; i += kThreads) {
+      float ya[8], yb[8];
+      int u, t, h;
+      const bool there = place(i, u, t, h);
+      T* y = static_cast<T*>(r.out) + (t0 + t) * r.out_row + (int64_t)h * r.out_head;
       const int j = u * 8, n = pairs - j;
-      float c[8], s[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) c[k] = cosines[t * padded + j + k], s[k] = sines[t * padded + j + k];
-      if constexpr (INTERLEAVED) {
-        mx_load8<TYPE>(x + 2 * j, 2 * n, a);
-        if (n > 4) mx_load8<TYPE>(x + 2 * j + 8, 2 * n - 8, b);
-        float ya[8], yb[8];
+      for (int k = 0; k < 8; ++k) ya[k] = a[k], yb[k] = b[k];
+      if (u < turned) {
+        float c[8], s[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          ya[2 * k] = __builtin_fmaf(a[2 * k], c[k], -(a[2 * k + 1] * s[k]));
-          ya[2 * k + 1] = __builtin_fmaf(a[2 * k + 1], c[k], a[2 * k] * s[k]);
-          yb[2 * k] = __builtin_fmaf(b[2 * k], c[k + 4], -(b[2 * k + 1] * s[k + 4]));
-          yb[2 * k + 1] = __builtin_fmaf(b[2 * k + 1], c[k + 4], b[2 * k] * s[k + 4]);
+        for (int k = 0; k < 8; ++k) c[k] = cosines[t * padded + j + k], s[k] = sines[t * padded + j + k];
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (k < n) {
+              ya[2 * k] = __builtin_fmaf(a[2 * k], c[k], -(a[2 * k + 1] * s[k]));
+              ya[2 * k + 1] = __builtin_fmaf(a[2 * k + 1], c[k], a[2 * k] * s[k]);
+            }
+            if (k + 4 < n) {
+              yb[2 * k] = __builtin_fmaf(b[2 * k], c[k + 4], -(b[2 * k + 1] * s[k + 4]));
+              yb[2 * k + 1] = __builtin_fmaf(b[2 * k + 1], c[k + 4], b[2 * k] * s[k + 4]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            ya[k] = __builtin_fmaf(a[k], c[k], -(b[k] * s[k]));
+            yb[k] = __builtin_fmaf(b[k], c[k], a[k] * s[k]);
+          }
         }
-        mx_store8<TYPE>(y + 2 * j, 2 * n, ya);
-        if (n > 4) mx_store8<TYPE>(y + 2 * j + 8, 2 * n - 8, yb);
-      } else {
-        mx_load8<TYPE>(x + j, n, a);
-        mx_load8<TYPE>(x + pairs + j, n, b);
-        float ya[8], yb[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          ya[k] = __builtin_fmaf(a[k], c[k], -(b[k] * s[k]));
-          yb[k] = __builtin_fmaf(b[k], c[k], a[k] * s[k]);
-        }
+      }
+      load(i + kThreads);
+      if (!there) continue;
+      if (!INTERLEAVED && u < turned) {
         mx_store8<TYPE>(y + j, n, ya);
         mx_store8<TYPE>(y + pairs + j, n, yb);
+      } else {
+        const int first = INTERLEAVED ? 2 * j : 2 * pairs + 16 * (u - turned);
+        mx_store8<TYPE>(y + first, r.dim - first, ya);
+        if (first + 8 < r.dim) mx_store8<TYPE>(y + first + 8, r.dim - first - 8, yb);
       }
     }
   }
@@ -116,7 +144,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs r, int tokens, 
 template <int TYPE>
 hipError_t launch(const RopeArgs& r, hipStream_t st) {
   const int padded = (r.pairs + 7) & ~7;
-  const int64_t units = padded / 8 + (r.dim - 2 * r.pairs + 15) / 16;
+  // (in place, what is not turned is where it belongs)
+  const bool in_place = r.out == r.x.data;
+  const int64_t units = r.interleaved ? (in_place ? padded / 8 : (r.dim + 15) / 16) : padded / 8 + (in_place ? 0 : (r.dim - 2 * r.pairs + 15) / 16);
+  if (!units) return hipSuccess;
   // Four tokens a workgroup share nothing but the launch; fewer where the grid would not fill the GPU, and then fewer heads.
   int tokens = 4;
   while (tokens > 1 && ((int64_t)tokens * padded > kRopeAngles || r.T / tokens < 1024)) tokens /= 2;
@@ -126,7 +157,8 @@ hipError_t launch(const RopeArgs& r, hipStream_t st) {
   const int groups = (r.heads + heads_each - 1) / heads_each;
   const int64_t tiles = ((int64_t)r.T + tokens - 1) / tokens * groups, most = max_blocks(kThreads);
   const dim3 grid((uint32_t)(tiles < most ? tiles : most));
-  return launch_kernel(r.interleaved ? rope_kernel<TYPE, true> : rope_kernel<TYPE, false>, grid, dim3(kThreads), 0, st, r, tokens, heads_each, groups, tiles);
+  return launch_kernel(r.interleaved ? rope_kernel<TYPE, true> : rope_kernel<TYPE, false>, grid, dim3(kThreads), 0, st, r, tokens, Divisor((uint32_t)heads_each),
+                       Divisor((uint32_t)units), (uint32_t)groups, tiles);
 }
 
 }  // namespace
