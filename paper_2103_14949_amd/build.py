@@ -27,9 +27,9 @@ HIPCC_FLAGS = [
 ]
 
 
-# Of single files.  The kernel for 256 columns of mx_attention_many.hip has 272 registers of sums and operands that vector instructions use; with the sums kept in the
+# Of single files.  The kernel for 256 columns in mx_attention_many_kernel.h has 272 registers of sums and operands that vector instructions use; with the sums kept in the
 # accumulation registers, as the compiler would, every one of them is copied (8192 tokens: 4.9 ms, and 0.9 without).
-FILE_FLAGS = {"mx_attention_many.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+FILE_FLAGS = dict.fromkeys(("mx_attention_many.hip", "mx_attention_many_f16.hip"), ["-mllvm", "-amdgpu-mfma-vgpr-form=1"])
 
 
 def sources():
@@ -166,7 +166,7 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
         _drain([(src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))], verbose)
 
     # first, so that none of them is waited for alone
-    slow = ("mx_attention_many.hip", "mx_attention.hip", "qgemm_dma_other.hip", "qgemm_line_other.hip", "qgemm_dma.hip", "qgemm_dma_clipped.hip", "conv_gather.hip", "dwconv.hip")
+    slow = ("mx_attention_many.hip", "mx_attention_many_f16.hip", "mx_attention.hip", "qgemm_dma_other.hip", "qgemm_line_other.hip", "qgemm_dma.hip", "qgemm_dma_clipped.hip", "conv_gather.hip", "dwconv.hip")
     with concurrent.futures.ThreadPoolExecutor(jobs) as pool:
         list(pool.map(lambda so: compile_one(*so), sorted(zip(sources(), objs), key=lambda so: not so[0].endswith(slow))))
     _check_assembly(objdir)

@@ -182,16 +182,15 @@ struct AttentionChunk {
 
 // Host side: blocks of 32 columns that the kernels are made for, and what the kernel for many rows has of rows and runs.
 constexpr int attention_blocks(int64_t dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
-template <int DB>
-constexpr int kManyGroups = 1;  // of 32 rows
-template <int DB>
-constexpr int kManyWaves = DB == 8 ? 4 : 8;
-constexpr int attention_many_rows(int db) { return 32 * (db == 2 ? kManyWaves<2> : db == 4 ? kManyWaves<4> : kManyWaves<8>); }
+// (two wavefronts a SIMD where 256 registers do)
+constexpr int attention_many_waves(int type, int db) { return type == kMxBf16 && db != 8 ? 8 : 4; }
+constexpr int attention_many_rows(int type, int db) { return 32 * attention_many_waves(type, db); }
 constexpr int attention_many_slots(int db) { return db == 8 ? 2 : 3; }  // (two of 256 columns take 141 KB)
 constexpr int kAttentionManyRuns = 256;
 // Whether a wavefront's `keys` neighbours, the first at a multiple of their number, lie in one page, and their scales in words of 32 bits that are the cache's.
 inline bool attention_even(const CacheArgs& c, int keys) { return c.page % keys == 0 && ptr_aligned(c.k_scales, 4) && ptr_aligned(c.v_scales, 4); }
-hipError_t launch_attention_many(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st);
+hipError_t launch_attention_many_bf16(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st);
+hipError_t launch_attention_many_f16(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st);
 
 constexpr float kAttentionLog2e = 1.44269504f, kAttentionLn2 = 0.693147181f;
 

@@ -393,9 +393,9 @@ hipError_t launch_join(const CacheArgs& c, const AttentionArgs& a, const Attenti
 template <int TYPE, int KF, int VF, int DB>
 hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
   const int group = a.heads / c.kv_heads;
-  if (TYPE == kMxBf16 && many_rows(a, c)) {
-    const hipError_t e = launch_attention_many(c, a, work, st);
-    return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(DB), 2 * kAttentionManyRuns, st);
+  if (TYPE != kMxF32 && many_rows(a, c)) {
+    const hipError_t e = TYPE == kMxBf16 ? launch_attention_many_bf16(c, a, work, st) : launch_attention_many_f16(c, a, work, st);
+    return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(TYPE, DB), 2 * kAttentionManyRuns, st);
   }
   const int64_t units = ((int64_t)a.T * group / kRows + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
   auto* kernel = attention_even(c, 16) ? attention_kernel<TYPE, KF, VF, DB, true> : attention_kernel<TYPE, KF, VF, DB, false>;
@@ -421,7 +421,7 @@ hipError_t with_formats(const CacheArgs& c, const AttentionArgs& a, const Attent
 // Rows of partials that a call can have.
 static int64_t partial_rows(int64_t T, int64_t heads, int64_t kv_heads, int db) {
   const int64_t few = 2ll * (db == 8 ? kRuns<8> : kRuns<4>) * kRows;
-  const int64_t many = 2ll * kAttentionManyRuns * attention_many_rows(db);
+  const int64_t many = 2ll * kAttentionManyRuns * attention_many_rows(kMxBf16, db);  // (the most of any type)
   return T * (heads / kv_heads) >= kManyRowsFrom && many > few ? many : few;
 }
 

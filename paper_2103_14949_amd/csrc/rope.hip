@@ -148,8 +148,8 @@ hipError_t launch(const RopeArgs& r, hipStream_t st) {
   const bool in_place = r.out == r.x.data;
   const int64_t units = r.interleaved ? (in_place ? padded / 8 : (r.dim + 15) / 16) : padded / 8 + (in_place ? 0 : (r.dim - 2 * r.pairs + 15) / 16);
   if (!units) return hipSuccess;
-  // Four tokens a workgroup share nothing but the launch; fewer where the grid would not fill the GPU, and then fewer heads.
-  int tokens = 4;
+  // Two tokens a workgroup (8192 x 40 x 128 bf16: 32.5 us, with four 33.2, with eight 35.2); one, and then fewer heads, where the grid would not fill the GPU.
+  int tokens = 2;
   while (tokens > 1 && ((int64_t)tokens * padded > kRopeAngles || r.T / tokens < 1024)) tokens /= 2;
   int heads_each = r.heads;
   while (heads_each > 1 && (int64_t)heads_each * tokens * units > kThreads && ((int64_t)r.T + tokens - 1) / tokens * ((r.heads + heads_each - 1) / heads_each) < 1024)
