@@ -92,18 +92,19 @@ struct AttentionRun {
 
 // Units are (ROWS rows, head); each is cut into ceil(blocks / share) runs, a block being BLOCK keys, such that there are about SHARES of them: at most
 // that many and as many as units, and of those of units that are cut at most twice as many.  Every wavefront finds the run for itself, 64 sequences
-// at a time.  (Offsets that break the contract can make counts wrap: what is found then is still inside its sequence.)
+// at a time; the sequence's rows and keys come with it.  (Offsets that break the contract can make counts wrap: what is found then is still inside its sequence.)
 template <int ROWS, int BLOCK, int SHARES>
-__device__ __forceinline__ bool attention_run(const CacheArgs& c, const AttentionArgs& a, uint32_t group, uint32_t id, AttentionRun& run) {
+__device__ __forceinline__ bool attention_run(const CacheArgs& c, const AttentionArgs& a, uint32_t group, uint32_t id, AttentionRun& run, AttentionSpan& span) {
   static_assert((SHARES & (SHARES - 1)) == 0);
   const int lane = threadIdx.x & 63;
+  AttentionSpan mine{};  // of this lane's sequence
   uint32_t units = 0, blocks = 1;
   const auto sizes = [&](int s) {
     units = 0, blocks = 1;
     if (s >= c.seqs) return;
-    const AttentionSpan span = attention_span(c, a, s);
-    units = ((uint32_t)span.rows * group + ROWS - 1) / ROWS * c.kv_heads;
-    if (span.high > span.low) blocks = (uint32_t)(span.high - (span.low & ~15) + BLOCK - 1) / BLOCK;
+    mine = attention_span(c, a, s);
+    units = ((uint32_t)mine.rows * group + ROWS - 1) / ROWS * c.kv_heads;
+    if (mine.high > mine.low) blocks = (uint32_t)(mine.high - (mine.low & ~15) + BLOCK - 1) / BLOCK;
   };
   uint64_t all = 0;
   for (int s = 0; s < c.seqs; s += 64) {
@@ -127,6 +128,12 @@ __device__ __forceinline__ bool attention_run(const CacheArgs& c, const Attentio
       run.local = (int)(id - before - __builtin_amdgcn_readlane(upto - count, at));
       run.runs = (int)__builtin_amdgcn_readlane(runs, at);
       run.slot = run.runs > 1 ? (int)(slots_before + __builtin_amdgcn_readlane(slots_upto - cut, at)) : -1;
+      span.first = __builtin_amdgcn_readlane(mine.first, at);
+      span.rows = __builtin_amdgcn_readlane(mine.rows, at);
+      span.low = __builtin_amdgcn_readlane(mine.low, at);
+      span.high = __builtin_amdgcn_readlane(mine.high, at);
+      const uint32_t below = __builtin_amdgcn_readlane((uint32_t)mine.position, at), above = __builtin_amdgcn_readlane((uint32_t)((uint64_t)mine.position >> 32), at);
+      span.position = (int64_t)((uint64_t)above << 32 | below);
       return true;
     }
     before += __builtin_amdgcn_readlane(upto, 63);

@@ -42,8 +42,8 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
   __shared__ __align__(16) uint8_t lds[kWaves * kRegion];
 
   AttentionRun run;
-  if (!attention_run<kRows, kBlock, kRuns<DB>>(c, a, group, blockIdx.x, run)) return;
-  const AttentionSpan span = attention_span(c, a, run.seq);
+  AttentionSpan span;
+  if (!attention_run<kRows, kBlock, kRuns<DB>>(c, a, group, blockIdx.x, run, span)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, part = lane / 16;
   // (rows of all heads: at most 2^27)
   const uint32_t all_rows = (uint32_t)span.rows * group, tiles = (all_rows + kRows - 1) / kRows;
@@ -323,22 +323,27 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
   __shared__ columns sums[PARTS - 1 ? PARTS - 1 : 1][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), part = PARTS == 1 ? 0 : wave;
   const int64_t first = (PARTS == 1 ? (int64_t)blockIdx.x * kWaves + wave : (int64_t)blockIdx.x) * each, mine = first + lane;
-  bool cut = lane < each && mine < rows;
+  bool cut = false;
   int2 whose = make_int2(0, 0);
-  if (cut) {
-    const int t = (int)((uint32_t)mine / (uint32_t)a.heads);  // (rows of all heads: at most 2^27)
-    cut = t >= c.offsets[0] && t < c.offsets[c.seqs];
-  }
-  if (cut) {
+  if (lane < each && mine < rows) {
     whose = work.joins[mine];
+    const int t = (int)((uint32_t)mine / (uint32_t)a.heads);  // (rows of all heads: at most 2^27)
     // (what no sequence wrote may be anything)
-    cut = whose.y >= 2 && whose.y <= kMostRuns && whose.x >= 0 && (int64_t)whose.x + (int64_t)apart * (whose.y - 1) < (int64_t)apart * slots;
+    cut = t >= c.offsets[0] && t < c.offsets[c.seqs] && whose.y >= 2 && whose.y <= kMostRuns && whose.x >= 0 &&
+          (int64_t)whose.x + (int64_t)apart * (whose.y - 1) < (int64_t)apart * slots;
   }
   for (uint64_t left = __ballot(cut); left; left &= left - 1) {
     const int at = __builtin_ctzll(left);
     const int64_t row = first + at;
     const int from = __builtin_amdgcn_readlane(whose.x, at), runs = __builtin_amdgcn_readlane(whose.y, at);
     const float2* stats = work.stats + from;
+    const float* partial = work.partial + (int64_t)from * D + lane * kColumns;
+    const auto partial_of = [&](int i) { return *reinterpret_cast<const columns*>(partial + (int64_t)apart * i * D); };
+    // the first partials are under way while the weights are worked out
+    constexpr int kEarly = 4;
+    columns early[kEarly];
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i) early[i] = part + i * PARTS < runs ? partial_of(part + i * PARTS) : columns{};
     float most = -INFINITY, sum = 0.0f;
     for (int i = lane; i < runs; i += 64) most = fmaxf(most, stats[(int64_t)apart * i].x);
 #pragma unroll
@@ -351,14 +356,16 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     columns y = {};
-    const float* partial = work.partial + (int64_t)from * D + lane * kColumns;
-#pragma unroll 4
-    for (int i = part; i < runs; i += PARTS) {
+    const auto add = [&](int i, const columns& p) {
       const float w = __builtin_amdgcn_exp2f(stats[(int64_t)apart * i].x - zero);
-      const columns p = *reinterpret_cast<const columns*>(partial + (int64_t)apart * i * D);
 #pragma unroll
       for (int k = 0; k < kColumns; ++k) y[k] = __builtin_fmaf(p[k], w, y[k]);
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i)
+      if (part + i * PARTS < runs) add(part + i * PARTS, early[i]);
+#pragma unroll 4
+    for (int i = part + kEarly * PARTS; i < runs; i += PARTS) add(i, partial_of(i));
     if constexpr (PARTS > 1) {
       if (part) sums[part - 1][lane] = y;
       __syncthreads();  // (all wavefronts go through the same rows)

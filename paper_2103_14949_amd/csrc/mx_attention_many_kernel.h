@@ -57,8 +57,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   Shared& shared = *reinterpret_cast<Shared*>(lds);
 
   AttentionRun run;
-  if (!attention_run<ROWS, kTile, kAttentionManyRuns>(c, a, group, blockIdx.x, run)) return;
-  const AttentionSpan span = attention_span(c, a, run.seq);
+  AttentionSpan span;
+  if (!attention_run<ROWS, kTile, kAttentionManyRuns>(c, a, group, blockIdx.x, run, span)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
   // (rows of all heads: at most 2^27)
   const uint32_t all_rows = (uint32_t)span.rows * group, tiles = (all_rows + ROWS - 1) / ROWS;
