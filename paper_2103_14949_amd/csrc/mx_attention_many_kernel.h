@@ -66,8 +66,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   const uint32_t unit = (uint32_t)run.local / (uint32_t)c.kv_heads;
   const int head = run.local - (int)unit * c.kv_heads, split = (int)(unit / tiles), tile = (int)(tiles - 1 - (unit - (uint32_t)split * tiles));
   const int blocks = (c.dim + 31) / 32;
-  // scores times a factor that is not negative: the queries take its sign
-  const float factor = fabsf(a.scale) * kAttentionLog2e;
+  // scores times a factor above zero (what a query does not see is minus infinity before it): the queries take its sign, and are zero where it is
+  const float factor = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kAttentionLog2e;
   const auto end_of = [&](int i) {
     const int64_t p = span.position + i + 1;
     return !a.causal || p > span.high ? span.high : p < 0 ? 0 : (int)p;
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
       for (int i = 0; i < 8; ++i) {
         const float v = row_there && 16 * st + 8 * half < c.dim ? (float)x[st][i] : 0.0f;
         __bf16 p[PIECES];
-        attention_split<PIECES>(a.scale < 0 ? -v : v, p);
+        attention_split<PIECES>(a.scale == 0.0f ? 0.0f : a.scale < 0 ? -v : v, p);
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) q[k][st][i] = p[k];
       }

@@ -93,3 +93,18 @@ def test_an_axis_that_is_none_has_position_zero():
     axis = torch.tensor([0, 1, 2, -1], dtype=torch.int32)
     got = hago.rope(x.to(DEV), pos.to(DEV), freq.to(DEV), axes=axis.to(DEV))
     assert torch.equal(got[..., [2, 3, 6, 7]].cpu(), x[..., [2, 3, 6, 7]])
+
+
+def test_beyond_32_bits():
+    """Rows whose elements lie behind 2^31."""
+    T, heads, dim = (1 << 20) + 3, 17, 128
+    x = torch.empty(T, heads, dim, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator().manual_seed(4)
+    last = torch.randn(5, heads, dim, generator=g).to(torch.bfloat16)
+    x[-5:] = last.to(DEV)
+    x[:5] = last.to(DEV)
+    pos = torch.arange(T, dtype=torch.int32)
+    freq = torch.pow(10000.0, -torch.arange(64) / 64).float()
+    got = hago.rope(x, pos.to(DEV), freq.to(DEV), out=x)
+    check(got[-5:], last, pos[None, -5:], freq, None, False, "bf16")
+    check(got[:5], last, pos[None, :5], freq, None, False, "bf16")
