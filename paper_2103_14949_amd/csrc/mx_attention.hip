@@ -4,12 +4,15 @@
 // out = softmax(scale * q k^T) v in one pass over the keys with the running maximum and sum.  The cache's bytes bound it, so a
 // workgroup is one (sequence, 16 rows, head of the cache) and a run of keys, its rows the queries of all heads that share those keys;
 // the runs are as long as makes all workgroups' work alike, whatever the lengths, and a second launch joins the sequences that were cut.
-// Lengths stay on the device: every workgroup finds its run by a scan over the sequences.
+// Lengths stay on the device: every wavefront finds its run by a scan over the sequences.
 //
 // A wavefront goes its own way through 32 keys at a time, with no barrier.  S^T = K Q^T: a lane (key r = lane % 16, part h = lane / 16)
-// loads part h of key r, which is whole in one block of 32 (or two) and becomes the operand by eight conversions.  Its results are keys
+// loads part h of key r, which is whole in one block of 32 (or two) and becomes the operand by conversions.  Its results are keys
 // 4 h .. 4 h + 3 of query r, which is the operand of O^T = V^T P^T as it stands, if V^T's lanes hold the same keys; they read them so from
-// LDS, 4 x 16 elements at a time transposed.
+// LDS, 4 x 16 elements at a time transposed.  Codes are an iteration ahead, the pages that they are in two.
+//
+// 64 sequences of 1024 to 16384 tokens, 32 heads over 8 of 128 columns, 8-bit codes: 146 us with the join's 7, 5.1 TB/s of 752 MB (a copy has 5.9); 4-bit codes 88 us.  One
+// token over 1000 keys 9.5 us, 6.5 and 3.8 of them the two kernels: launches, and three rounds of memory in the first.
 #include "mx_attention.h"
 
 namespace hago {
@@ -17,7 +20,8 @@ namespace hago {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kRows = 16, kKeys = 32, kBlock = kWaves * kKeys;
-// Workgroups that share the keys, by blocks of a row: as many as are resident.
+// Workgroups that share the keys, by blocks of a row: about three times what is resident, so that the last ones are short (the 64 sequences above with 1024, 2048 and
+// 4096 of them: 167, 158 and 173 us when each began more slowly).
 template <int DB>
 constexpr int kRuns = DB == 8 ? 1024 : 2048;
 constexpr int kMostRuns = 2048;
@@ -314,7 +318,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
 
 // Joins the runs of a row, whose partials are `apart` rows apart: by the four wavefronts of a workgroup where there are few rows (PARTS 4; a long sequence's token has up
 // to a run a CU), by one where there are many.  The order of the sums is the runs' in either.  A wavefront looks at `each` rows together for those that were cut:
-// none of a long prompt's, whose units are many (a workgroup for every row of 8192 x 32 took 120 us to find nothing).
+// none of a long prompt's, whose units are many (a workgroup for every row of 8192 x 32 took 110 us to find nothing; this takes 4.6).
 template <int TYPE, int DB, int PARTS>
 __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, int64_t rows, int each, int apart, int slots) {
   using E = typename MxElement<TYPE>::type;
@@ -383,8 +387,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
   }
 }
 
-// Which kernel: the one for many rows where a sequence has this many on the average, queries of all heads that share keys.
-constexpr int64_t kManyRowsFrom = 64;
+// Which kernel: the one for many rows where a sequence has more than two tiles of sixteen on the average, queries of all heads that share keys (the number of rows of
+// each is not known here).  16 sequences of 4096, 16, 32, 48, 64 and 128 rows of 128 columns, us: bfloat16 44, 57, 76, 85, 152 here and 56, 60, 58, 60, 71 there; float16 51, 66,
+// 86, 95, 159 and 72, 75, 76, 76, 94.  Short sequences gain later: 64 chunks of 64 rows with nothing before them 28 and 38, of 256 rows 76 and 47.
+// binary32 queries take three products for one and have the kernel here alone.
+constexpr int64_t kManyRowsFrom = 33;
 bool many_rows(const AttentionArgs& a, const CacheArgs& c) { return (int64_t)a.T * (a.heads / c.kv_heads) >= kManyRowsFrom * c.seqs; }
 
 constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }

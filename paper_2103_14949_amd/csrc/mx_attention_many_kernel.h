@@ -1,10 +1,16 @@
 // Attention over a paged cache of microscaled keys and values, many rows a sequence: chunks and prompts.
 //
-// The matrix unit bounds it.  A workgroup is one (sequence, tile of rows, head of the cache) and a run of keys; its rows are the queries of all heads
-// that share those keys, 32 a wavefront.  Keys and values of 64 positions at a time become bfloat16 once for all of them, on their way from
-// memory through registers into LDS, two tiles deep with one barrier a tile; the conversions are hidden behind the products.  S^T = K Q^T leaves a
+// The matrix unit bounds it, and beside it the exponentials (four issue slots each on the same SIMD).  A workgroup is one (sequence, tile of rows, head of the cache) and a
+// run of keys; its rows are the queries of all heads that share those keys, 32 a wavefront.  Keys and values of 64 positions at a time become
+// bfloat16 once for all of them, on their way from memory through registers into LDS, with one barrier a tile.  S^T = K Q^T leaves a
 // query's scores in two lanes' registers, as the operand of O^T = V^T P^T, so that the softmax needs one lane exchange and nothing of it goes
-// through LDS; values are read transposed from there.
+// through LDS; values are read transposed from there.  The next tile's scores are worked out beside this tile's exponentials, in the order that is written.
+//
+// Eight wavefronts of 32 rows share a CU, two a SIMD, up to 128 columns of bfloat16; four where 256 registers do not do.  Prompt of 8192, 32 heads over 8 of 128 columns: 540 to 566 us,
+// 970 to 1020 TFLOP/s (a product of 8192 x 8192 x 8192 has 1480, of 16384 1600), matrix unit 44 % of the cycles at 2 GHz, vector instructions 56 %; a chunk of 1024 over 32768 503 to 528 us; 256 columns
+// 595 TFLOP/s, float16 queries 430.  Tried and slower: 64 rows a wavefront, whose sums the compiler copies between register files (1020 us); three tiles in LDS and the
+// first operands read in front of the barrier (registers: 595 for 555); eight operands ahead (660 for 590).  LDS is not what bounds it: half the operand reads, on the same
+// data twice, 634 us for 652.
 #pragma once
 
 #include "mx_attention.h"
@@ -342,6 +348,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
             exponentials(e - 1);
           }
       };
+      // a wavefront that has its exponentials under way goes first on its SIMD: the two are not at the same place then (prompt of 8192 579 -> 566 us)
+      __builtin_amdgcn_s_setprio(1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = kLead; k < kProducts; ++k) {
@@ -369,6 +377,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
       most = pair_max(most);
       if (any_none) {
         // NaN for the queries that see such a value, and for no other: block d lies in part d PARTS / DB

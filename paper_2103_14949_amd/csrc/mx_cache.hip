@@ -2,7 +2,11 @@
 //
 // Both move bytes.  A lane takes eight consecutive columns of a row's keys and of its values, a quad of lanes a block of 32 (as in the
 // other operators by rows).  A workgroup takes consecutive tokens of one head: they are neighbours in a page, so that its codes and
-// its scales, four bytes a row at 128 columns, leave as whole lines, and a row of the tensors is 256 bytes together anyway.
+// its scales, four bytes a row at 128 columns, leave as whole lines, and a row of the tensors is 256 bytes together anyway.  Where a row lies (its
+// sequence, page, place) is found by one thread for all lanes of it, while the tensors' loads are under way.
+//
+// Four prompts of 8954 tokens in all, 8 heads of 128 columns, with values: 16.8 us, 5.2 TB/s; 131072 tokens read back: 145 us, 5.6 TB/s (a copy has 5.9).  One, two and four
+// rows a thread: 17.9, 16.8 and 19.3 us, and 158 (191 with every lane looking for itself), 146 and 156.
 #include "mx_cache_device.h"
 
 namespace hago {
@@ -129,8 +133,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(CacheArgs c, void* k, vo
   }
 }
 
-// Several launches where one would hold too many threads.  EACH: as many rows a thread as leave a workgroup a row of places a thread, and the GPU
-// four workgroups a CU
+// Several launches where one would hold too many threads.
 template <class Each>
 hipError_t by_tiles(const CacheArgs& c, int64_t T, int rows, Each&& each) {
   const int64_t tiles = (T + rows - 1) / rows * c.kv_heads, most = max_blocks(kThreads);
@@ -138,6 +141,7 @@ hipError_t by_tiles(const CacheArgs& c, int64_t T, int rows, Each&& each) {
   for (int64_t first = 0; first < tiles && e == hipSuccess; first += most) e = each(dim3((uint32_t)(tiles - first < most ? tiles - first : most)), first);
   return e;
 }
+// Two rows a thread where that leaves eight workgroups a CU.
 constexpr int kRowsAThread = 2, kManyTiles = 2048;
 bool many_rows(const CacheArgs& c, int64_t T, int rows) { return (T + rows * kRowsAThread - 1) / (rows * kRowsAThread) * c.kv_heads >= kManyTiles; }
 

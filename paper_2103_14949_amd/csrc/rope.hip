@@ -4,6 +4,9 @@
 // many as give every thread something, works out each token's cosines and sines once (one pair a thread), and keeps them in LDS.  An
 // angle far from the origin loses its fraction in 32 bits: position * frequency, its turns and their fraction are 64 bits, the
 // polynomials behind them 32.
+//
+// 8192 x 40 heads x 128 columns, bf16, from a strided tensor: 32.5 us, 5.2 TB/s (a copy has 5.9); 4001 x 20 x 80 f16 on three axes 9.3 us (13.5 with loads of single elements at the ends of the
+// pairs); one token 4.4 us, the host's.
 #include "mx_cache.h"
 #include "mx_device.h"
 
