@@ -18,6 +18,9 @@
  *   hago_mx_quantize, hago_mx_rmsnorm, hago_mx_silu_mul, hago_mx_dense,
  *   hago_mx_dense_grouped -- microscaled (block-scaled) 4- and 8-bit floating
  *                          point: a transformer's layers on codes
+ *   hago_rope, hago_mx_cache_write, hago_mx_cache_read, hago_mx_attention --
+ *                          rotary positions, a paged cache of keys and values
+ *                          on microscaled codes, attention over it
  * and the operand / accumulator variants the paper names: int16 x int16
  * operands, 24-bit accumulators (Sec. 4.1), shift-only requantize for
  * power-of-two scales (Sec. 5.1).
@@ -27,9 +30,10 @@
  *     device; "host" are ordinary pointers.  The caller owns every buffer it
  *     passes: the library never frees or keeps such a pointer after returning.
  *   - No entry point allocates, frees or keeps device memory, and none waits
- *     for the device.  The one operator that wants scratch memory, the
+ *     for the device.  The two operators that want scratch memory, the
  *     groups == 1 convolution (it rewrites its operands before the matrix
- *     cores read them), takes it from the caller: hago_qconv2d_ws.
+ *     cores read them) and the attention (runs of keys meet there), take it
+ *     from the caller: hago_qconv2d_ws, hago_mx_attention.
  *   - A call is kernel launches on `stream` and nothing else, so it may be
  *     recorded into a HIP graph.  The first call that reaches a kernel with a
  *     large LDS footprint raises that kernel's limit on the current device
