@@ -618,16 +618,18 @@ hago_status hago_mx_cache_read(const hago_mx_cache* cache,
  * Codes and their scales go into the products as bfloat16, which holds them
  * (below 2^-126 they may count as zero); queries and probabilities as one, two or
  * three bfloat16 numbers for HAGO_BF16, HAGO_F16 and HAGO_F32; sums are binary32,
- * of probabilities up to 2^6 (values of 2^120 and more may leave its range).
+ * of probabilities up to 2^6 (values of 2^120 and queries of 2^127 and more may
+ * leave its range).
  * workspace: device, 256-byte aligned, hago_mx_attention_workspace_bytes(...) bytes at
  * least, of any contents; calls that may run at the same time need one each.
  * Errors: as above, and SHAPE (heads not a multiple of kv_heads, T * heads beyond
  * 2^27, seqs * kv_heads beyond 2^22; window negative), PARAM (scale
- * not finite; workspace too small or misaligned).
+ * NaN or beyond 2^100; workspace too small or misaligned).
  * hago_mx_attention_workspace_bytes returns -1 for what the call would refuse.
  */
-int64_t hago_mx_attention_workspace_bytes(int64_t T, int64_t heads,
-                                          int64_t kv_heads, int64_t dim);
+int64_t hago_mx_attention_workspace_bytes(int64_t T, int64_t seqs,
+                                          int64_t heads, int64_t kv_heads,
+                                          int64_t dim);
 hago_status hago_mx_attention(const hago_mx_cache* cache,
                               const hago_mx_sequences* sequences, const void* q,
                               hago_dtype q_t, int64_t T, int64_t heads,

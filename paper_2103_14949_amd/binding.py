@@ -127,7 +127,7 @@ def lib():
         L.hago_mx_cache_read.restype = i32
         L.hago_mx_cache_read.argtypes = [cache, seqs, i32, i64, vp, vp, vp]
         L.hago_mx_attention_workspace_bytes.restype = i64
-        L.hago_mx_attention_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.hago_mx_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
         L.hago_mx_attention.restype = i32
         L.hago_mx_attention.argtypes = [cache, seqs, vp, i32, i64, i64, i64, i64, C.c_float, i32, i64, vp, vp, vp, i64, vp]
         L.hago_bit_range.restype = i32
@@ -422,9 +422,9 @@ def mx_cache_read(cache: MXCache, table, lengths, offsets, rows, out_dtype=BF16,
     return (_native or _native_module()).mx_cache_read(cache, table, lengths, offsets, rows, out_dtype, out, prepare)
 
 
-def mx_attention_workspace_bytes(T, heads, kv_heads, dim):
+def mx_attention_workspace_bytes(T, seqs, heads, kv_heads, dim):
     """hago_mx_attention_workspace_bytes."""
-    return int(lib().hago_mx_attention_workspace_bytes(int(T), int(heads), int(kv_heads), int(dim)))
+    return int(lib().hago_mx_attention_workspace_bytes(int(T), int(seqs), int(heads), int(kv_heads), int(dim)))
 
 
 def mx_attention(q, cache: MXCache, table, lengths, offsets, scale=None, causal=True, window=0, lse=False, out=None, workspace=None, prepare=False):

@@ -72,6 +72,7 @@ struct AttentionWork {
   float* partial;   // [slots][rows of a tile][32 DB]
   float2* stats;    // [slots][rows of a tile]: maximum and sum
   int2* joins;      // [T][heads]: the row of the first of its partials, number of partials
+  uint32_t* plan;   // NULL, or [seqs + 1][2]: keys of a run in blocks, then runs and partials of all sequences up to each
 };
 
 // Sums over the lanes up to each.
@@ -90,35 +91,74 @@ struct AttentionRun {
   int seq, local, runs, slot;  // place among the sequence's runs, runs of a unit, first partial of the sequence (-1: none)
 };
 
-// Units are (ROWS rows, head); each is cut into ceil(blocks / share) runs, a block being BLOCK keys, such that there are about SHARES of them: at most
-// that many and as many as units, and of those of units that are cut at most twice as many.  Every wavefront finds the run for itself, 64 sequences
-// at a time; the sequence's rows and keys come with it.  (Offsets that break the contract can make counts wrap: what is found then is still inside its sequence.)
-template <int ROWS, int BLOCK, int SHARES>
-__device__ __forceinline__ bool attention_run(const CacheArgs& c, const AttentionArgs& a, uint32_t group, uint32_t id, AttentionRun& run, AttentionSpan& span) {
+// A sequence's units (ROWS rows, head) and their keys in blocks of BLOCK; none behind the last sequence.
+template <int ROWS, int BLOCK>
+__device__ __forceinline__ void attention_units(const CacheArgs& c, const AttentionArgs& a, uint32_t group, int seq, AttentionSpan& span, uint32_t& units, uint32_t& blocks) {
+  units = 0, blocks = 1;
+  if (seq >= c.seqs) return;
+  span = attention_span(c, a, seq);
+  units = ((uint32_t)span.rows * group + ROWS - 1) / ROWS * c.kv_heads;
+  if (span.high > span.low) blocks = (uint32_t)(span.high - (span.low & ~15) + BLOCK - 1) / BLOCK;
+}
+template <int SHARES>
+__device__ __forceinline__ uint32_t attention_share(uint64_t all) {
   static_assert((SHARES & (SHARES - 1)) == 0);
+  const uint64_t wide = (all + SHARES - 1) / SHARES;
+  return __builtin_amdgcn_readfirstlane(wide > 0x7fffffffu ? 0x7fffffffu : wide ? (uint32_t)wide : 1);
+}
+
+// Units are cut into ceil(blocks / share) runs, such that there are about SHARES of them: at most
+// that many and as many as units, and of those of units that are cut at most twice as many.  Every wavefront finds the run for itself, 64 sequences
+// at a time, or in the plan that a launch in front has made of many sequences; the sequence's rows and keys come with it.  (Offsets that break the
+// contract can make counts wrap: what is found then is still inside its sequence.)
+template <int ROWS, int BLOCK, int SHARES>
+__device__ __forceinline__ bool attention_run(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, uint32_t group, uint32_t id, AttentionRun& run,
+                                              AttentionSpan& span) {
   const int lane = threadIdx.x & 63;
+  if (work.plan) {
+    const uint32_t* const ends = work.plan + 2;
+    int low = 0, high = c.seqs;  // the first sequence whose runs end behind id is among them, if it is any
+    while (high - low > 1) {
+      const int step = (high - low + 63) / 64, at = low + (lane + 1) * step - 1 < high ? low + (lane + 1) * step - 1 : high - 1;
+      const uint64_t behind = __ballot(ends[2 * (int64_t)at] > id);
+      if (!behind) return false;
+      const int first = __builtin_ctzll(behind), from = low + first * step;
+      high = from + step < high ? from + step : high;
+      low = from;
+    }
+    low = __builtin_amdgcn_readfirstlane(low);
+    const uint32_t before = low ? ends[2 * (int64_t)low - 2] : 0, slots_before = low ? ends[2 * (int64_t)low - 1] : 0, share = work.plan[0];
+    uint32_t units, blocks;
+    AttentionSpan found;
+    attention_units<ROWS, BLOCK>(c, a, group, low, found, units, blocks);
+    const uint32_t runs = blocks > share ? (blocks + share - 1) / share : 1, local = id - before;
+    if (__builtin_amdgcn_readfirstlane(local >= units * runs)) return false;
+    run.seq = low;
+    run.local = (int)__builtin_amdgcn_readfirstlane(local);
+    run.runs = (int)__builtin_amdgcn_readfirstlane(runs);
+    run.slot = run.runs > 1 ? (int)__builtin_amdgcn_readfirstlane(slots_before) : -1;
+    span.first = __builtin_amdgcn_readfirstlane(found.first);
+    span.rows = __builtin_amdgcn_readfirstlane(found.rows);
+    span.low = __builtin_amdgcn_readfirstlane(found.low);
+    span.high = __builtin_amdgcn_readfirstlane(found.high);
+    const uint32_t below = __builtin_amdgcn_readfirstlane((uint32_t)found.position), above = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)found.position >> 32));
+    span.position = (int64_t)((uint64_t)above << 32 | below);
+    return true;
+  }
   AttentionSpan mine{};  // of this lane's sequence
   uint32_t units = 0, blocks = 1;
-  const auto sizes = [&](int s) {
-    units = 0, blocks = 1;
-    if (s >= c.seqs) return;
-    mine = attention_span(c, a, s);
-    units = ((uint32_t)mine.rows * group + ROWS - 1) / ROWS * c.kv_heads;
-    if (mine.high > mine.low) blocks = (uint32_t)(mine.high - (mine.low & ~15) + BLOCK - 1) / BLOCK;
-  };
   uint64_t all = 0;
   for (int s = 0; s < c.seqs; s += 64) {
-    sizes(s + lane);
+    attention_units<ROWS, BLOCK>(c, a, group, s + lane, mine, units, blocks);
     all += (uint64_t)units * blocks;
   }
   if (c.seqs > 1)
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
-  const uint64_t wide = (all + SHARES - 1) / SHARES;
-  const uint32_t share = __builtin_amdgcn_readfirstlane(wide > 0x7fffffffu ? 0x7fffffffu : wide ? (uint32_t)wide : 1);
+  const uint32_t share = attention_share<SHARES>(all);
   uint32_t before = 0, slots_before = 0;
   for (int s = 0; s < c.seqs; s += 64) {
-    if (c.seqs > 64) sizes(s + lane);
+    if (c.seqs > 64) attention_units<ROWS, BLOCK>(c, a, group, s + lane, mine, units, blocks);
     const uint32_t runs = blocks > share ? (blocks + share - 1) / share : 1, count = units * runs, cut = runs > 1 ? count : 0;
     const uint32_t upto = attention_scan(count), slots_upto = attention_scan(cut);
     const uint64_t found = __ballot(id - before - (upto - count) < count);
@@ -141,6 +181,57 @@ __device__ __forceinline__ bool attention_run(const CacheArgs& c, const Attentio
   }
   return false;
 }
+
+namespace {  // (a kernel of its own in every file)
+
+// The plan of more sequences than every wavefront should look at, by one workgroup.
+constexpr int kPlanThreads = 1024;
+template <int ROWS, int BLOCK, int SHARES>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(CacheArgs c, AttentionArgs a, uint32_t* plan, uint32_t group) {
+  constexpr int kPlanWaves = kPlanThreads / 64;
+  __shared__ uint64_t totals[kPlanWaves];
+  __shared__ uint2 counts[kPlanWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+  AttentionSpan span;
+  uint32_t units, blocks;
+  uint64_t all = 0;
+  for (int64_t s = tid; s < c.seqs; s += kPlanThreads) {
+    attention_units<ROWS, BLOCK>(c, a, group, (int)s, span, units, blocks);
+    all += (uint64_t)units * blocks;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
+  if (lane == 0) totals[wave] = all;
+  __syncthreads();
+  all = 0;
+  for (int w = 0; w < kPlanWaves; ++w) all += totals[w];
+  const uint32_t share = attention_share<SHARES>(all);
+  if (tid == 0) plan[0] = share;
+  uint32_t before = 0, slots_before = 0;
+  for (int64_t base = 0; base < c.seqs; base += kPlanThreads) {
+    const int64_t s = base + tid;
+    attention_units<ROWS, BLOCK>(c, a, group, s < c.seqs ? (int)s : c.seqs, span, units, blocks);
+    const uint32_t runs = blocks > share ? (blocks + share - 1) / share : 1, count = units * runs, cut = runs > 1 ? count : 0;
+    const uint32_t upto = attention_scan(count), slots_upto = attention_scan(cut);
+    if (lane == 63) counts[wave] = make_uint2(upto, slots_upto);
+    __syncthreads();
+    uint32_t earlier = before, slots_earlier = slots_before;
+    for (int w = 0; w < kPlanWaves; ++w) {
+      const uint2 n = counts[w];
+      if (w < wave) earlier += n.x, slots_earlier += n.y;
+      before += n.x, slots_before += n.y;
+    }
+    if (s < c.seqs) plan[2 + 2 * s] = earlier + upto, plan[3 + 2 * s] = slots_earlier + slots_upto;
+    __syncthreads();
+  }
+}
+template <int ROWS, int BLOCK, int SHARES>
+hipError_t launch_plan(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
+  if (!work.plan) return hipSuccess;
+  return launch_kernel(plan_kernel<ROWS, BLOCK, SHARES>, dim3(1), dim3(kPlanThreads), 0, st, c, a, work.plan, (uint32_t)(a.heads / c.kv_heads));
+}
+
+}  // namespace
 
 // A lane's part of a key or value: 8 DB codes.
 template <int FORMAT, int DB>

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
 
   AttentionRun run;
   AttentionSpan span;
-  if (!attention_run<kRows, kBlock, kRuns<DB>>(c, a, group, blockIdx.x, run, span)) return;
+  if (!attention_run<kRows, kBlock, kRuns<DB>>(c, a, work, group, blockIdx.x, run, span)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, part = lane / 16;
   // (rows of all heads: at most 2^27)
   const uint32_t all_rows = (uint32_t)span.rows * group, tiles = (all_rows + kRows - 1) / kRows;
@@ -394,6 +394,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
 constexpr int64_t kManyRowsFrom = 33;
 bool many_rows(const AttentionArgs& a, const CacheArgs& c) { return (int64_t)a.T * (a.heads / c.kv_heads) >= kManyRowsFrom * c.seqs; }
 
+// More sequences are planned by a launch in front.  With every workgroup looking at all of them, tokens over 512 sequences of 512, 2048 of 1024 and 4096 of 64 keys took 152, 1172 and
+// 1973 us; so 115, 770 and 272, and the launch 5 of those.
+constexpr int64_t kMostScanned = 256;
+
 constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }
 
 template <int TYPE, int DB>
@@ -412,6 +416,7 @@ hipError_t launch(const CacheArgs& c, const AttentionArgs& a, const AttentionWor
     return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, attention_many_rows(TYPE, DB), 2 * kAttentionManyRuns, st);
   }
   const int64_t units = ((int64_t)a.T * group / kRows + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
+  if (const hipError_t e = launch_plan<kRows, kBlock, kRuns<DB>>(c, a, work, st); e != hipSuccess) return e;
   auto* kernel = attention_even(c, 16) ? attention_kernel<TYPE, KF, VF, DB, true> : attention_kernel<TYPE, KF, VF, DB, false>;
   const hipError_t e = launch_kernel(kernel, dim3((uint32_t)(units + kRuns<DB>)), dim3(kThreads), 0, st, c, a, work, (uint32_t)group);
   return e != hipSuccess ? e : launch_join<TYPE, DB>(c, a, work, kRows, 2 * kRuns<DB>, st);
@@ -439,9 +444,10 @@ static int64_t partial_rows(int64_t T, int64_t heads, int64_t kv_heads, int db) 
   return T * (heads / kv_heads) >= kManyRowsFrom && many > few ? many : few;
 }
 
-int64_t mx_attention_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t dim) {
+int64_t mx_attention_workspace_bytes(int64_t T, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim) {
   const int db = attention_blocks(dim);
-  return partial_rows(T, heads, kv_heads, db) * (32 * db * 4 + (int64_t)sizeof(float2)) + padded16(T * heads * (int64_t)sizeof(int2));
+  return partial_rows(T, heads, kv_heads, db) * (32 * db * 4 + (int64_t)sizeof(float2)) + padded16(T * heads * (int64_t)sizeof(int2)) +
+         (seqs > kMostScanned ? (seqs + 1) * 2 * (int64_t)sizeof(uint32_t) : 0);
 }
 
 hipError_t launch_mx_attention(const CacheArgs& c, const AttentionArgs& a, void* workspace, hipStream_t st) {
@@ -452,6 +458,8 @@ hipError_t launch_mx_attention(const CacheArgs& c, const AttentionArgs& a, void*
   work.partial = reinterpret_cast<float*>(w);
   work.stats = reinterpret_cast<float2*>(w + rows * 32 * db * 4);
   work.joins = reinterpret_cast<int2*>(w + rows * (32 * db * 4 + (int64_t)sizeof(float2)));
+  const int64_t plan = rows * (32 * db * 4 + (int64_t)sizeof(float2)) + padded16((int64_t)a.T * a.heads * (int64_t)sizeof(int2));
+  work.plan = c.seqs > kMostScanned ? reinterpret_cast<uint32_t*>(w + plan) : nullptr;
   return a.type == kMxF32 ? with_formats<kMxF32>(c, a, work, st) : a.type == kMxBf16 ? with_formats<kMxBf16>(c, a, work, st) : with_formats<kMxF16>(c, a, work, st);
 }
 

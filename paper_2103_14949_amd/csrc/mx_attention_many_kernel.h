@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
 
   AttentionRun run;
   AttentionSpan span;
-  if (!attention_run<ROWS, kTile, kAttentionManyRuns>(c, a, group, blockIdx.x, run, span)) return;
+  if (!attention_run<ROWS, kTile, kAttentionManyRuns>(c, a, work, group, blockIdx.x, run, span)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
   // (rows of all heads: at most 2^27)
   const uint32_t all_rows = (uint32_t)span.rows * group, tiles = (all_rows + ROWS - 1) / ROWS;
@@ -517,6 +517,7 @@ hipError_t launch_even(const CacheArgs& c, const AttentionArgs& a, const Attenti
   if (const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), (int)bytes, raised); e != hipSuccess) return e;
   const int group = a.heads / c.kv_heads;
   const int64_t units = ((int64_t)a.T * group / ROWS + (c.seqs < a.T ? c.seqs : a.T)) * c.kv_heads;
+  if (const hipError_t e = launch_plan<ROWS, kTile, kAttentionManyRuns>(c, a, work, st); e != hipSuccess) return e;
   return launch_kernel(kernel, dim3((uint32_t)(units + kAttentionManyRuns)), dim3(64 * WAVES), bytes, st, c, a, work, (uint32_t)group);
 }
 template <int TYPE, int KF, int VF, int DB, int WAVES>

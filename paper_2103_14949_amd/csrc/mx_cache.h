@@ -48,7 +48,7 @@ struct AttentionArgs {
   int32_t T, heads, causal, window;  // window 0: none
   int32_t type;
 };
-int64_t mx_attention_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t dim);
+int64_t mx_attention_workspace_bytes(int64_t T, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim);
 hipError_t launch_mx_attention(const CacheArgs& c, const AttentionArgs& a, void* workspace, hipStream_t st);
 
 struct RopeArgs {

@@ -127,11 +127,12 @@ hago_status hago_mx_cache_read(const hago_mx_cache* cache, const hago_mx_sequenc
   return from_hip(hago::launch_mx_cache_read(c, real_type(out_t), T, k, v, static_cast<hipStream_t>(stream)));
 }
 
-int64_t hago_mx_attention_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t dim) {
-  if (T < 0 || heads < 0 || kv_heads < 0 || kv_heads > kMostHeads || dim < 0 || dim > hago::kCacheMostDim || !product_fits(T, heads, hago::kMostRows) ||
+int64_t hago_mx_attention_workspace_bytes(int64_t T, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim) {
+  if (T < 0 || seqs < 0 || heads < 0 || kv_heads < 0 || kv_heads > kMostHeads || dim < 0 || dim > hago::kCacheMostDim || !product_fits(T, heads, hago::kMostRows) || !product_fits(seqs, kv_heads, hago::kMostUnits) ||
+      seqs > kI32Max - 1 ||
       (kv_heads ? heads % kv_heads : heads) != 0)
     return -1;
-  return T && heads && dim ? hago::mx_attention_workspace_bytes(T, heads, kv_heads, dim) : 0;
+  return T && heads && dim ? hago::mx_attention_workspace_bytes(T, seqs, heads, kv_heads, dim) : 0;
 }
 
 hago_status hago_mx_attention(const hago_mx_cache* cache, const hago_mx_sequences* sequences, const void* q, hago_dtype q_t, int64_t T, int64_t heads,
@@ -141,10 +142,10 @@ hago_status hago_mx_attention(const hago_mx_cache* cache, const hago_mx_sequence
   bool empty = true;
   const hago_status s = check_cache(cache, sequences, T, q_t, empty, c);
   if (s != HAGO_OK) return s;
-  const int64_t need = hago_mx_attention_workspace_bytes(T, heads, cache->kv_heads, cache->dim);
-  if (need < 0 || window < 0 || !product_fits(sequences->seqs, cache->kv_heads, hago::kMostUnits) || !strides_fit(T, heads, q_row_stride, q_head_stride))
+  const int64_t need = hago_mx_attention_workspace_bytes(T, sequences->seqs, heads, cache->kv_heads, cache->dim);
+  if (need < 0 || window < 0 || !strides_fit(T, heads, q_row_stride, q_head_stride))
     return HAGO_ERR_SHAPE;
-  if (!std::isfinite(scale)) return HAGO_ERR_PARAM;
+  if (!(std::fabs(scale) <= 0x1p100f)) return HAGO_ERR_PARAM;  // (NaN too)
   if (empty || heads == 0) return HAGO_OK;
   if (!q || !out || !workspace) return HAGO_ERR_NULL;
   const size_t size = real_size(q_t);

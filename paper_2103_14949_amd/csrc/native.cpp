@@ -956,7 +956,7 @@ PyObject* f_mx_attention(PyObject* const* a, Py_ssize_t n) {
   if (has_lse && a[8] != Py_True) tensor(a[8]), given(a[8], at::IntArrayRef(shape, 2), at::kFloat), on_current_device({a[8]});
   given(a[9], at::IntArrayRef(shape, 3), q.scalar);
   m.on_device({a[0], a[9], a[10]});
-  int64_t bytes = L.hago_mx_attention_workspace_bytes(q.T, q.heads, m.cache.kv_heads, q.dim);
+  int64_t bytes = L.hago_mx_attention_workspace_bytes(q.T, m.sequences.seqs, q.heads, m.cache.kv_heads, q.dim);
   if (a[10] != Py_None) {
     const at::Tensor& w = tensor(a[10]);
     require(w.scalar_type() == at::kByte && w.is_contiguous() && w.numel() >= bytes);

@@ -59,6 +59,7 @@ int main() {
       {"prompt wide", [&] { return attend(HAGO_F16, 512, 32, 8, 256, 1, 64); }},
       {"prompt f32", [&] { return attend(HAGO_F32, 8192, 32, 8, 128, 1, 64); }},
       {"chunks of sixteen rows", [&] { return attend(HAGO_BF16, 64, 32, 8, 128, 16, 64); }},
+      {"many chunks", [&] { return attend(HAGO_BF16, 257 * 20, 32, 8, 128, 257, 64); }},
       {"most rows", [&] { return attend(HAGO_BF16, 1 << 27, 1, 1, 128, 1 << 22, 64); }},
       {"most tokens", [&] { return attend(HAGO_F32, 1 << 27, 1, 1, 128, 1 << 22, 64); }},
   };

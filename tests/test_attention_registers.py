@@ -15,7 +15,7 @@ def test_no_vector_register_is_spilled():
         pytest.skip("no assembly here: the libraries were built elsewhere")
     with open(paths[0]) as f:
         text = f.read()
-    kernels = re.findall(r"\.name:\s+(\S+).*?\.vgpr_spill_count:\s+(\d+)", text, re.S)
+    kernels = [k for k in re.findall(r"\.name:\s+(\S+).*?\.vgpr_spill_count:\s+(\d+)", text, re.S) if "many_kernel" in k[0]]
     assert len(kernels) == 24 and max(int(spilled) for _, spilled in kernels) <= 16
     assert [k for k, spilled in kernels if int(spilled) and re.search(r"Li[24]ELi8ELb1E", k)] == []
 

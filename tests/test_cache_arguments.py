@@ -107,14 +107,15 @@ def test_write_and_read(L):
 
 def test_attention(L):
     bytes = L.hago_mx_attention_workspace_bytes
-    assert bytes(5, 4, 2, 64) > 0 and bytes(0, 4, 2, 64) == 0 and bytes(1, 8, 2, 256) > bytes(1, 8, 2, 64)
-    for bad in ((-1, 4, 2, 64), (5, -4, 2, 64), (5, 4, -2, 64), (5, 5, 2, 64), (5, 4, 0, 64), (5, 4, 2, 257), (2 ** 26, 4, 2, 64), (5, 4, 65537, 64)):
+    assert bytes(5, 3, 4, 2, 64) > 0 and bytes(0, 3, 4, 2, 64) == 0 and bytes(1, 1, 8, 2, 256) > bytes(1, 1, 8, 2, 64) and bytes(5, 1000, 4, 2, 64) > bytes(5, 3, 4, 2, 64)
+    for bad in ((-1, 3, 4, 2, 64), (5, -1, 4, 2, 64), (5, 3, -4, 2, 64), (5, 3, 4, -2, 64), (5, 3, 5, 2, 64), (5, 3, 4, 0, 64), (5, 3, 4, 2, 257), (2 ** 26, 3, 4, 2, 64),
+                (5, 3, 4, 65537, 64), (5, 2 ** 21 + 1, 4, 2, 64)):
         assert bytes(*bad) == -1, bad
     assert attend(L, q=None) == NULL and attend(L, out=None) == NULL and attend(L, ws=None) == NULL
     for bad in (dict(heads=5), dict(heads=-4), dict(window=-1), dict(row=-1), dict(head=-1), dict(row=2 ** 61), dict(T=2 ** 26)):
         assert attend(L, **bad) == SHAPE, bad
     assert attend(L, s=sequences(seqs=2 ** 21 + 1)) == SHAPE
-    for bad in (dict(scale=math.inf), dict(scale=math.nan), dict(q=P + 1), dict(out=P + 1), dict(lse=P + 2), dict(ws=P + 128), dict(bytes=bytes(5, 4, 2, 64) - 1)):
+    for bad in (dict(scale=math.inf), dict(scale=math.nan), dict(scale=-2e30), dict(q=P + 1), dict(out=P + 1), dict(lse=P + 2), dict(ws=P + 128), dict(bytes=bytes(5, 3, 4, 2, 64) - 1)):
         assert attend(L, **bad) == PARAM, bad
     assert attend(L, heads=0, q=None, out=None, ws=None) == 0
 

@@ -224,7 +224,7 @@ def test_a_workspace_of_any_contents():
     q = torch.randn(6, 4, 64, device=DEV, dtype=torch.float16)
     want = hago.mx_attention(q, cache, *where)
     for byte in (0, 0x7F, 0xFF):
-        room = torch.full((hago.mx_attention_workspace_bytes(6, 4, 1, 64),), byte, dtype=torch.uint8, device=DEV)
+        room = torch.full((hago.mx_attention_workspace_bytes(6, 2, 4, 1, 64),), byte, dtype=torch.uint8, device=DEV)
         assert torch.equal(hago.mx_attention(q, cache, *where, workspace=room), want)
 
 

@@ -141,3 +141,35 @@ def test_beyond_32_bits(new, page):
         hago.mx_cache_write(cache, k, v, *where, *on_gpu(np.array([0, total], np.int32)))
         outs.append(hago.mx_attention(q, cache, *where, *on_gpu(np.array([0, new], np.int32))))
     assert torch.equal(*outs) and outs[0].isfinite().all()
+
+
+@pytest.mark.parametrize("most", [2, 60])
+@pytest.mark.parametrize("seqs", [257, 1024, 1025, 3000])
+def test_a_plan_of_many_sequences(seqs, most):
+    """More sequences than every workgroup looks at: the same as in calls of a hundred, bit by bit where none is cut."""
+    rng = np.random.default_rng(seqs)
+    new = rng.integers(0, most, seqs)
+    lengths = np.minimum(new + rng.integers(0, 9, seqs), 64)
+    table, lengths, offsets, pages = layout(list(new), list(lengths), 16, seed=seqs)
+    cache, _, _ = random_cache(rng, pages, 2, 16, 64, "fp8", "fp4")
+    q = torch.randn(int(offsets[-1]), 4, 64, device=DEV, dtype=torch.bfloat16)
+    got, lse = hago.mx_attention(q, cache, *on_gpu(table, lengths, offsets), lse=True)
+    for first in range(0, seqs, 100):
+        end = min(first + 100, seqs)
+        a, b = int(offsets[first]), int(offsets[end])
+        part = hago.mx_attention(q[a:b], cache, *on_gpu(table[first:end], lengths[first:end], offsets[first:end + 1] - a), lse=True)
+        assert torch.equal(got[a:b], part[0]) and torch.equal(lse[a:b], part[1])
+
+
+def test_a_plan_with_long_sequences():
+    """Some of many are cut."""
+    new, lengths = [1] * 300, [3] * 300
+    lengths[7], lengths[299] = 30000, 9000
+    run(new, lengths, 2, 1, 32, 64, seed=13)
+    offsets = [[0, 300, 5], [-3, 2 ** 31 - 1]]   # and offsets that break the contract, with as many
+    cache = hago.MXCache.empty(8, 1, 16, 32)
+    q = torch.randn(400, 2, 32, device=DEV, dtype=torch.bfloat16)
+    for bad in offsets:
+        off = np.resize(np.array(bad, np.int32), 301)
+        hago.mx_attention(q, cache, *on_gpu(np.zeros((300, 2), np.int32), np.full(300, 30, np.int32), off))
+    torch.cuda.synchronize()
