@@ -617,7 +617,9 @@ hago_status hago_mx_cache_read(const hago_mx_cache* cache,
  * zeros, and -infinity there.  q has rows and heads at any distance, out is dense.
  * Codes and their scales go into the products as bfloat16, which holds them
  * (below 2^-126 they may count as zero); queries and probabilities as one, two or
- * three bfloat16 numbers for HAGO_BF16, HAGO_F16 and HAGO_F32; sums are binary32,
+ * three bfloat16 numbers for HAGO_BF16, HAGO_F16 and HAGO_F32, but two of a
+ * probability for HAGO_BF16 too in calls of few rows (T * heads / kv_heads less than
+ * 33 * seqs); sums are binary32,
  * of probabilities up to 2^6 (values of 2^120 and queries of 2^127 and more may
  * leave its range).
  * workspace: device, 256-byte aligned, hago_mx_attention_workspace_bytes(...) bytes at

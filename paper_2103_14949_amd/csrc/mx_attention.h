@@ -1,8 +1,8 @@
 // What the kernels of the attention over a paged cache of microscaled keys and values have in common.
 //
 // Keys and values go into the matrix instructions as bfloat16, which holds every code times its scale (three bits of mantissa, the
-// exponents of binary32; below 2^-126 it may be zero); queries and probabilities as one, two or three bfloat16 numbers that add up to
-// theirs: bfloat16 queries are held by one, float16 by two, binary32 by three.  Sums are binary32.
+// exponents of binary32; below 2^-126 it may be zero); queries as one, two or three bfloat16 numbers that add up to theirs (bfloat16, float16, binary32), and probabilities
+// as each kernel says.  Sums are binary32.
 #pragma once
 
 #include "mx_cache_device.h"

@@ -9,7 +9,9 @@
 // A wavefront goes its own way through 32 keys at a time, with no barrier.  S^T = K Q^T: a lane (key r = lane % 16, part h = lane / 16)
 // loads part h of key r, which is whole in one block of 32 (or two) and becomes the operand by conversions.  Its results are keys
 // 4 h .. 4 h + 3 of query r, which is the operand of O^T = V^T P^T as it stands, if V^T's lanes hold the same keys; they read them so from
-// LDS, 4 x 16 elements at a time transposed.  Codes are an iteration ahead, the pages that they are in two.
+// LDS, 4 x 16 elements at a time transposed.  Codes are an iteration ahead, the pages that they are in two.  Probabilities are two
+// bfloat16 numbers for bfloat16 queries too: one would be 2^-8 off, as much as the result's own rounding, and the second costs 0 to 2.5 % where bytes bound the kernel
+// (the 64 sequences below 148.1 and 148.6 us, their 4-bit codes 89.1 and 91.5).
 //
 // 64 sequences of 1024 to 16384 tokens, 32 heads over 8 of 128 columns, 8-bit codes: 146 us with the join's 7, 5.1 TB/s of 752 MB (a copy has 5.9); 4-bit codes 88 us.  One
 // token over 1000 keys 9.5 us, 6.5 and 3.8 of them the two kernels: launches, and three rounds of memory in the first.
@@ -38,7 +40,7 @@ __device__ __forceinline__ float sum_of_parts(float v) {
 template <int TYPE, int KF, int VF, int DB, bool EVEN>
 __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void attention_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, uint32_t group) {
   using E = typename MxElement<TYPE>::type;
-  constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB;
+  constexpr int PIECES = kAttentionPieces<TYPE>, PROBABILITIES = TYPE == kMxF32 ? 3 : 2, D = 32 * DB;
   constexpr int kRow = 2 * D + 32;                          // bytes of a row of values in LDS: 4 x 16 elements of it fall on different banks
   constexpr int kSums = D + 4;                              // floats of a row of results there
   constexpr int kRegion = kKeys * kRow;                     // of a wavefront
@@ -226,17 +228,17 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
     const float fade = __builtin_amdgcn_exp2f(m - zero);
     m = most;
     l *= fade;
-    at_b8 pr[PIECES];
+    at_b8 pr[PROBABILITIES];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float p = __builtin_amdgcn_exp2f(x[i][j] - zero);
         l += p;
-        __bf16 piece[PIECES];
-        attention_split<PIECES>(p, piece);
+        __bf16 piece[PROBABILITIES];
+        attention_split<PROBABILITIES>(p, piece);
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) pr[k][4 * i + j] = piece[k];
+        for (int k = 0; k < PROBABILITIES; ++k) pr[k][4 * i + j] = piece[k];
       }
     // O^T
 #pragma unroll
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(kThreads, TYPE != kMxBf16 && DB == 8 ? 1 : 2) void 
       for (int i = 0; i < 2; ++i)
         v.half[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)(mine + (16 * i + 4 * part + r / 4) * kRow + 32 * d + 8 * (r % 4)));
 #pragma unroll
-      for (int p = PIECES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.whole, pr[p], o[d], 0, 0, 0);
+      for (int p = PROBABILITIES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.whole, pr[p], o[d], 0, 0, 0);
     }
     if (any) {
       // NaN for the queries that see such a value, and for no other: tile d is columns 16 d on, which part 2 d / DB holds
