@@ -320,11 +320,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
           for (int e = 0; e < 16; ++e) o[d][e] *= fade;
       }
       const float zero = m == -INFINITY ? 0.0f : -m;
+      // The product in the exponent is not rounded, the maximum's was: half a step of m apart, which 2^16 keeps at 2^-8.  Larger scores are rounded like the maximum.
+      const bool far = __ballot(fabsf(zero) >= 0x1p16f);
+      if (far) [[unlikely]] {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) s.s[e / 16][e % 16] *= factor;
+      }
+      const float times = far ? 1.0f : factor;
       mx_u4 pr[PIECES][4];
       float x[2];
       const auto exponentials = [&](int e) {  // elements e and e + 1
 #pragma unroll
-        for (int j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s.s[(e + j) / 16][(e + j) % 16], factor, zero));
+        for (int j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s.s[(e + j) / 16][(e + j) % 16], times, zero));
         asm volatile("" : "+v"(x[0]), "+v"(x[1]));  // (here, not where they are used)
       };
       const auto probabilities = [&](int e) {
