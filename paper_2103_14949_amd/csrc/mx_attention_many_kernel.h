@@ -39,26 +39,36 @@ __device__ __forceinline__ float pair_sum(float v) {
   return p.x + p.y;
 }
 
+// Bytes of a row in LDS: neighbours on different banks, as they are read.
+constexpr int many_key_row(int db) { return 64 * db + 16; }
+constexpr int many_value_row(int db) { return 64 * db + 64; }
+
+// A workgroup's LDS; rows are written sixteen bytes at a time.  WAVES threads load a value, each one or two blocks of it.
+template <int DB, int WAVES>
+struct ManyShared {
+  static constexpr int kScales = AttentionChunk<kMxFp8, 4 * DB / WAVES>::kScales;
+  struct Values {
+    alignas(16) uint8_t rows[kTile * many_value_row(DB)];
+    uint64_t none[kScales][WAVES];  // bit WAVES * (key % kKeysAWave) + part: the part's block of a value stands for NaN
+    uint64_t gone[WAVES];           // the key has no place
+    uint8_t flags[8];               // of the wavefronts that loaded it: 1: some key is gone, 2: some block is NaN
+  };
+  alignas(16) uint8_t keys[2][kTile * many_key_row(DB)];
+  Values values[2];
+};
+
 template <int TYPE, int KF, int VF, int DB, int WAVES, bool EVEN>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, uint32_t group) {
   constexpr int slots = 2 * kAttentionManyRuns;
   using E = typename MxElement<TYPE>::type;
   constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * WAVES, STEPS = 2 * DB, kProducts = 2 * STEPS, kAhead = 4, kLead = kProducts / 4;
-  constexpr int kKeyRow = 2 * D + 16, kValueRow = 2 * D + 64;  // bytes in LDS: neighbours on different banks, as they are read
+  constexpr int kKeyRow = many_key_row(DB), kValueRow = many_value_row(DB);
   constexpr int PARTS = THREADS / kTile, kChunk = 4 * DB / PARTS;   // threads that load a key, and a value
   constexpr int kKeysAWave = 64 / PARTS;
   using KeyChunk = AttentionChunk<KF, kChunk>;
   using ValueChunk = AttentionChunk<VF, kChunk>;
-  struct Values {
-    uint8_t rows[kTile * kValueRow];
-    uint64_t none[ValueChunk::kScales][WAVES];  // bit PARTS * (key % kKeysAWave) + part: the part's block of a value stands for NaN
-    uint64_t gone[WAVES];                       // the key has no place
-    uint8_t flags[8];                           // of the wavefronts that loaded it: 1: some key is gone, 2: some block is NaN
-  };
-  struct Shared {
-    uint8_t keys[2][kTile * kKeyRow];
-    Values values[2];
-  };
+  using Shared = ManyShared<DB, WAVES>;
+  using Values = typename Shared::Values;
   extern __shared__ __align__(16) uint8_t lds[];
   Shared& shared = *reinterpret_cast<Shared*>(lds);
 
@@ -516,8 +526,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
 
 template <int TYPE, int KF, int VF, int DB, int WAVES, bool EVEN>
 hipError_t launch_even(const CacheArgs& c, const AttentionArgs& a, const AttentionWork& work, hipStream_t st) {
-  constexpr int D = 32 * DB, ROWS = 32 * WAVES;
-  constexpr size_t bytes = 2 * (kTile * (4 * D + 80) + 24 * WAVES + 8);
+  constexpr int ROWS = 32 * WAVES;
+  using Shared = ManyShared<DB, WAVES>;
+  constexpr size_t bytes = sizeof(Shared);
+  static_assert(many_key_row(DB) % 16 == 0 && many_value_row(DB) % 16 == 0 && sizeof(typename Shared::Values) % 16 == 0, "whole vectors");
+  static_assert(bytes <= 160 * 1024);
   static_assert(ROWS == attention_many_rows(TYPE, DB), "partials are laid out by it");
   auto* kernel = many_kernel<TYPE, KF, VF, DB, WAVES, EVEN>;
   static std::atomic<uint64_t> raised{0};

@@ -1,0 +1,25 @@
+"""The attention's kernels for many rows as they were built, of bfloat16 and float16 queries."""
+import glob
+import os
+import re
+
+import pytest
+
+from paper_2103_14949_amd import build
+
+FILES = ["mx_attention_many", "mx_attention_many_f16"]
+
+
+def assembly(name):
+    paths = glob.glob(os.path.join(os.path.dirname(build.LIB), "_build", name + "-*gfx950.s"))
+    if not paths:
+        pytest.skip("no assembly here: the libraries were built elsewhere")
+    with open(paths[0]) as f:
+        return f.read()
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_rows_in_lds_are_written_whole(name):
+    """Sixteen bytes at an address of sixteen: where the compiler sees another, it writes two halves."""
+    text = assembly(name)
+    assert "ds_write_b128" in text and "ds_write2_b64" not in text and "ds_write2st64_b64" not in text
