@@ -283,7 +283,6 @@ constexpr int attention_blocks(int64_t dim) { return dim <= 64 ? 2 : dim <= 128 
 // (two wavefronts a SIMD where 256 registers do)
 constexpr int attention_many_waves(int type, int db) { return type == kMxBf16 && db != 8 ? 8 : 4; }
 constexpr int attention_many_rows(int type, int db) { return 32 * attention_many_waves(type, db); }
-constexpr int attention_many_slots(int db) { return db == 8 ? 2 : 3; }  // (two of 256 columns take 141 KB)
 constexpr int kAttentionManyRuns = 256;
 // Whether a wavefront's `keys` neighbours, the first at a multiple of their number, lie in one page, and their scales in words of 32 bits that are the cache's.
 inline bool attention_even(const CacheArgs& c, int keys) { return c.page % keys == 0 && ptr_aligned(c.k_scales, 4) && ptr_aligned(c.v_scales, 4); }
