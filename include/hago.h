@@ -627,7 +627,9 @@ hago_status hago_mx_cache_read(const hago_mx_cache* cache,
  * Errors: as above, and SHAPE (heads not a multiple of kv_heads, T * heads beyond
  * 2^27, seqs * kv_heads beyond 2^22; window negative), PARAM (scale
  * NaN or beyond 2^100; workspace too small or misaligned).
- * hago_mx_attention_workspace_bytes returns -1 for what the call would refuse.
+ * hago_mx_attention_workspace_bytes returns -1 for what the call would refuse.  What
+ * it returns does not fall where T or seqs rise: room for the largest call, in both,
+ * serves every smaller one of the same heads and columns, whichever kernel that has.
  */
 int64_t hago_mx_attention_workspace_bytes(int64_t T, int64_t seqs,
                                           int64_t heads, int64_t kv_heads,

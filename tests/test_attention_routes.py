@@ -46,3 +46,15 @@ def test_some_of_their_sequences_are_cut(case):
     runs = [-(-b // share) for u, b in zip(units, blocks) if u]
     assert max(runs) > 1
     assert len(case["new"]) == 1 or case in CUT or min(runs) == 1
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(32, 8, 128), (4, 4, 64), (16, 1, 256)])
+def test_room_for_the_largest_call_serves_the_smaller_ones(serve, heads, kv_heads, dim):
+    """Whichever kernel each of them has: the size does not fall where tokens or sequences rise, and a call takes as much as the size says."""
+    sizes = [(T, seqs) for T in (1, 8, 9, 32, 33, 64, 300, 5000) for seqs in (1, 2, 64, 256, 257, 300)]
+    bytes_of = {s: hago.mx_attention_workspace_bytes(*s, heads, kv_heads, dim) for s in sizes}
+    for a in sizes:
+        assert all(bytes_of[b] >= bytes_of[a] for b in sizes if b[0] >= a[0] and b[1] >= a[1])
+    got = serve([(t, T, heads, kv_heads, dim, seqs, 64) for t in (0, 1, 2) for T, seqs in sizes])
+    assert [n for _, n in got] == 3 * [bytes_of[s] for s in sizes]
+    assert {"many_kernel" in k[-2] for k, _ in got} == {True, False}
