@@ -618,8 +618,8 @@ hago_status hago_mx_cache_read(const hago_mx_cache* cache,
  * Codes and their scales go into the products as bfloat16, which holds them
  * (below 2^-126 they may count as zero); queries and probabilities as one, two or
  * three bfloat16 numbers for HAGO_BF16, HAGO_F16 and HAGO_F32, but two of a
- * probability for HAGO_BF16 too in calls of few rows (T * heads / kv_heads less than
- * 33 * seqs); sums are binary32,
+ * probability for HAGO_BF16 too, save calls of many rows (T * heads / kv_heads 33 *
+ * seqs or more) and up to 128 columns; sums are binary32,
  * of probabilities up to 2^6 (values of 2^120, queries and scores of 2^127 and more may
  * leave its range).  Scores may be large otherwise: the largest of a row's counts.
  * workspace: device, 256-byte aligned, hago_mx_attention_workspace_bytes(...) bytes at

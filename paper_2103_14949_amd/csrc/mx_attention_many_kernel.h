@@ -39,6 +39,12 @@ __device__ __forceinline__ float pair_sum(float v) {
   return p.x + p.y;
 }
 
+// bfloat16 numbers that a probability is in the second product: two, which hold it to 2^-16; but one, 2^-8, in bfloat16 calls of up to 128 columns, whose loop the matrix
+// unit and the vector instructions take turns in.  There the second would cost 38 % (prompt of 8192 536 -> 743 us, 64 columns 385 -> 504), where the rounding makes the error against
+// 64 bits 1.35 times that of the result's own (0.00223 and 0.00166 of it); of 256 columns it costs 8 % (793 -> 857).  Float16 numbers, which are as fast as one, hold no
+// probabilities below 2^-24, of which a result may be made where the values beside them are zero.
+constexpr int many_probabilities(int type, int db) { return type == kMxBf16 && db != 8 ? 1 : 2; }
+
 // Bytes of a row in LDS: neighbours on different banks, as they are read.
 constexpr int many_key_row(int db) { return 64 * db + 16; }
 constexpr int many_value_row(int db) { return 64 * db + 64; }
@@ -61,7 +67,7 @@ template <int TYPE, int KF, int VF, int DB, int WAVES, bool EVEN>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, uint32_t group) {
   constexpr int slots = 2 * kAttentionManyRuns;
   using E = typename MxElement<TYPE>::type;
-  constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * WAVES, STEPS = 2 * DB, kProducts = 2 * STEPS, kAhead = 4, kLead = kProducts / 4;
+  constexpr int PIECES = kAttentionPieces<TYPE>, PROBABILITIES = many_probabilities(TYPE, DB), D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * WAVES, STEPS = 2 * DB, kProducts = 2 * STEPS, kAhead = 4, kLead = kProducts / 4;
   constexpr int kKeyRow = many_key_row(DB), kValueRow = many_value_row(DB);
   constexpr int PARTS = THREADS / kTile, kChunk = 4 * DB / PARTS;   // threads that load a key, and a value
   constexpr int kKeysAWave = 64 / PARTS;
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
         for (int e = 0; e < 32; ++e) s.s[e / 16][e % 16] *= factor;
       }
       const float times = far ? 1.0f : factor;
-      mx_u4 pr[PIECES][4];
+      mx_u4 pr[PROBABILITIES][4];
       float x[2];
       const auto exponentials = [&](int e) {  // elements e and e + 1
 #pragma unroll
@@ -346,11 +352,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
       };
       const auto probabilities = [&](int e) {
         l += x[0] + x[1];
-        __bf16 piece[2][PIECES];
+        __bf16 piece[2][PROBABILITIES];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) attention_split<PIECES>(x[j], piece[j]);
+        for (int j = 0; j < 2; ++j) attention_split<PROBABILITIES>(x[j], piece[j]);
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
+        for (int k = 0; k < PROBABILITIES; ++k) {
           uint32_t pair = __builtin_bit_cast(uint32_t, at_b2{piece[0][k], piece[1][k]});
           asm volatile("" : "+v"(pair), "+v"(l));
           pr[k][e / 8][e % 8 / 2] = pair;
@@ -379,7 +385,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
       for (int k = 0; k < kProducts; ++k) {
         const int u = k / DB, d = k % DB;
 #pragma unroll
-        for (int p = PIECES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values[k % kAhead], __builtin_bit_cast(at_b8, pr[p][u]), o[d], 0, 0, 0);
+        for (int p = PROBABILITIES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values[k % kAhead], __builtin_bit_cast(at_b8, pr[p][u]), o[d], 0, 0, 0);
         if (k + kAhead < kProducts) values[k % kAhead] = value_of(turn, k + kAhead);
         if (k < kLead) some(k + kProducts - kLead);
         if (k == kLead) probabilities(30);

@@ -34,3 +34,10 @@ def off(new, lengths, heads, kv_heads, dim, seed, probability):
 def test_few_rows(new, lengths, dim):
     """Probabilities of two bfloat16 numbers: 2^-16."""
     assert off(new, lengths, 8, 4, dim, dim, 2.0 ** -16).max() <= 1
+
+
+@pytest.mark.parametrize("dim", [129, 200, 256])
+@pytest.mark.parametrize("new,lengths", [([70, 9], [70, 40]), ([33, 40], [700, 33]), ([40], [5000])])
+def test_many_rows_of_more_than_128_columns(new, lengths, dim):
+    """The same in the kernel for many rows."""
+    assert off(new, lengths, 8, 4, dim, dim, 2.0 ** -16).max() <= 1
