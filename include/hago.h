@@ -616,12 +616,13 @@ hago_status hago_mx_cache_read(const hago_mx_cache* cache,
  * heads], unless NULL, takes log(sum_j e^(s_j)).  A row that sees nothing gives
  * zeros, and -infinity there.  q has rows and heads at any distance, out is dense.
  * Codes and their scales go into the products as bfloat16, which holds them
- * (below 2^-126 they may count as zero); queries and probabilities as one, two or
- * three bfloat16 numbers for HAGO_BF16, HAGO_F16 and HAGO_F32, but two of a
- * probability for HAGO_BF16 too, save calls of many rows (T * heads / kv_heads 33 *
- * seqs or more) and up to 128 columns; sums are binary32,
- * of probabilities up to 2^6 (values of 2^120, queries and scores of 2^127 and more may
- * leave its range).  Scores may be large otherwise: the largest of a row's counts.
+ * (below 2^-126 they may count as zero); queries as one, two or three bfloat16 numbers
+ * for HAGO_BF16, HAGO_F16 and HAGO_F32, probabilities as two, two and three: 2^-16,
+ * 2^-16 and 2^-24 of each.  HAGO_BF16 calls of many rows (T * heads / kv_heads 33 * seqs
+ * or more) and up to 128 columns hold a probability to 2^-11, and those below 2^-27 of a
+ * row's largest to 2^-38 of that.  Sums are binary32, of probabilities up to 2^6 where
+ * values are large (values of 2^120, queries and scores of 2^127 and more may leave its
+ * range).  Scores may be large otherwise: the largest of a row's counts.
  * workspace: device, 256-byte aligned, hago_mx_attention_workspace_bytes(...) bytes at
  * least, of any contents; calls that may run at the same time need one each.
  * Errors: as above, and SHAPE (heads not a multiple of kv_heads, T * heads beyond

@@ -272,10 +272,10 @@ struct AttentionChunk {
 #pragma unroll
     for (int i = 0; i < kScales; ++i) scale[i] = scale[i] >> shift[i] & 255;
   }
-  // eight codes of step st
-  __device__ __forceinline__ at_b8 values(int st) const {
-    return attention_values8<FORMAT>(w + st * (FORMAT == kMxFp4 ? 1 : 2), __builtin_bit_cast(float, scale[st / 4 % kScales] << 23));
-  }
+  // eight codes of step st, and 2^up times their scale
+  __device__ __forceinline__ const uint32_t* words(int st) const { return w + st * (FORMAT == kMxFp4 ? 1 : 2); }
+  __device__ __forceinline__ float scale_of(int st, int up) const { return __builtin_bit_cast(float, (scale[st / 4 % kScales] + up) << 23); }
+  __device__ __forceinline__ at_b8 values(int st) const { return attention_values8<FORMAT>(words(st), scale_of(st, 0)); }
 };
 
 // Host side: blocks of 32 columns that the kernels are made for, and what the kernel for many rows has of rows and runs.

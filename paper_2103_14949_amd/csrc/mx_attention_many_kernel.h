@@ -2,7 +2,7 @@
 //
 // The matrix unit bounds it, and beside it the exponentials (four issue slots each on the same SIMD).  A workgroup is one (sequence, tile of rows, head of the cache) and a
 // run of keys; its rows are the queries of all heads that share those keys, 32 a wavefront.  Keys and values of 64 positions at a time become
-// bfloat16 once for all of them, on their way from memory through registers into LDS, with one barrier a tile.  S^T = K Q^T leaves a
+// bfloat16 (values float16, see many_halves) once for all of them, on their way from memory through registers into LDS, with one barrier a tile.  S^T = K Q^T leaves a
 // query's scores in two lanes' registers, as the operand of O^T = V^T P^T, so that the softmax needs one lane exchange and nothing of it goes
 // through LDS; values are read transposed from there.  The next tile's scores are worked out beside this tile's exponentials, in the order that is written.
 //
@@ -20,6 +20,8 @@ namespace hago {
 namespace {
 
 typedef float at_f16 __attribute__((ext_vector_type(16)));
+typedef _Float16 at_h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 at_h8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 64;  // keys
 
@@ -39,15 +41,43 @@ __device__ __forceinline__ float pair_sum(float v) {
   return p.x + p.y;
 }
 
-// bfloat16 numbers that a probability is in the second product: two, which hold it to 2^-16; but one, 2^-8, in bfloat16 calls of up to 128 columns, whose loop the matrix
-// unit and the vector instructions take turns in.  There the second would cost 38 % (prompt of 8192 536 -> 743 us, 64 columns 385 -> 504), where the rounding makes the error against
-// 64 bits 1.35 times that of the result's own (0.00223 and 0.00166 of it); of 256 columns it costs 8 % (793 -> 857).  Float16 numbers, which are as fast as one, hold no
-// probabilities below 2^-24, of which a result may be made where the values beside them are zero.
-constexpr int many_probabilities(int type, int db) { return type == kMxBf16 && db != 8 ? 1 : 2; }
-
 // Bytes of a row in LDS: neighbours on different banks, as they are read.
 constexpr int many_key_row(int db) { return 64 * db + 16; }
 constexpr int many_value_row(int db) { return 64 * db + 64; }
+
+// In the second product a probability is two bfloat16 numbers, which hold it to 2^-16.  In bfloat16 calls of up to 128 columns, whose loop the matrix unit and the vector
+// instructions take turns in, the second would cost 38 % (prompt of 8192 536 -> 743 us, 64 columns 385 -> 504; of 256 columns 8 %), and one alone made the error against 64 bits 1.35 times that of
+// the result's own rounding (0.00223 and 0.00166 of it).  There the product is one of float16 numbers, which hold a probability to 2^-11: 2^kHead times the probability, so
+// that those down to 2^-27 of the largest have all their bits and those down to 2^-30 the eight of the result, and up to 2^kSlack times that.  Values are in it 2^kValuesUp times theirs,
+// exactly, if the scale of their block, so much higher, lies between 2^narrow_low and 2^narrow_high: blocks whose largest magnitude is at least 2^-12 (8 bits; 2^-26 with 4) and below 2^11.  A
+// run of keys that meets another block begins again, with two bfloat16 numbers and no tile ahead (prompt of 8192 800 to 830 us, wherever the block is).
+constexpr bool many_halves(int type, int db) { return type == kMxBf16 && db != 8; }
+constexpr int kValuesUp = 5;
+constexpr float kHead = 13.0f;
+// (E4M3: 2^-9 to 448, E2M1: 2^-1 to 6; float16: 2^-24 to 65504)
+constexpr int narrow_low(int format) { return format == kMxFp4 ? -23 : -15; }
+constexpr int narrow_high(int format) { return format == kMxFp4 ? 13 : 7; }
+
+// Eight codes of a block as float16: dwords `w` (fp8: two, fp4: one), scale 2^(byte - 127).
+template <int FORMAT>
+__device__ __forceinline__ at_h8 attention_halves8(const uint32_t* w, float scale) {
+  at_h2 d[4];
+  if constexpr (FORMAT == kMxFp4) {
+    d[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[0], scale, 0);
+    d[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[0], scale, 1);
+    d[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[0], scale, 2);
+    d[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[0], scale, 3);
+  } else {
+    d[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[0], scale, false);
+    d[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[0], scale, true);
+    d[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[1], scale, false);
+    d[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[1], scale, true);
+  }
+  at_h8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = d[i / 2][i % 2];
+  return v;
+}
 
 // A workgroup's LDS; rows are written sixteen bytes at a time.  WAVES threads load a value, each one or two blocks of it.
 template <int DB, int WAVES>
@@ -57,7 +87,7 @@ struct ManyShared {
     alignas(16) uint8_t rows[kTile * many_value_row(DB)];
     uint64_t none[kScales][WAVES];  // bit WAVES * (key % kKeysAWave) + part: the part's block of a value stands for NaN
     uint64_t gone[WAVES];           // the key has no place
-    uint8_t flags[8];               // of the wavefronts that loaded it: 1: some key is gone, 2: some block is NaN
+    uint8_t flags[8];               // of the wavefronts that loaded it: 1: some key is gone, 2: some block is NaN, 4: float16 does not hold some block
   };
   alignas(16) uint8_t keys[2][kTile * many_key_row(DB)];
   Values values[2];
@@ -67,7 +97,7 @@ template <int TYPE, int KF, int VF, int DB, int WAVES, bool EVEN>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c, AttentionArgs a, AttentionWork work, uint32_t group) {
   constexpr int slots = 2 * kAttentionManyRuns;
   using E = typename MxElement<TYPE>::type;
-  constexpr int PIECES = kAttentionPieces<TYPE>, PROBABILITIES = many_probabilities(TYPE, DB), D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * WAVES, STEPS = 2 * DB, kProducts = 2 * STEPS, kAhead = 4, kLead = kProducts / 4;
+  constexpr int PIECES = kAttentionPieces<TYPE>, D = 32 * DB, THREADS = 64 * WAVES, ROWS = 32 * WAVES, STEPS = 2 * DB, kProducts = 2 * STEPS, kAhead = 4, kLead = kProducts / 4;
   constexpr int kKeyRow = many_key_row(DB), kValueRow = many_value_row(DB);
   constexpr int PARTS = THREADS / kTile, kChunk = 4 * DB / PARTS;   // threads that load a key, and a value
   constexpr int kKeysAWave = 64 / PARTS;
@@ -203,110 +233,110 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
     if (EVEN && st == 0) kc.unpack(key_shift);
     *reinterpret_cast<at_b8*>(shared.keys[turn] + loader_key * kKeyRow + part * 16 * kChunk + 16 * st) = kc.values(st);
   };
-  // Values of a tile before they go to LDS.  What has no place, and what is NaN, is zero there: a probability of zero does not take a NaN away
-  const auto prepare_values = [&](int turn, int base, bool page_there) {
-    Values& v = shared.values[turn];
-    constexpr int kScales = ValueChunk::kScales;
-    if (EVEN) vc.unpack(value_shift);
-    bool none = false;
-#pragma unroll
-    for (int s = 0; s < kScales; ++s) none |= vc.scale[s] == 255;
-    const bool there = page_there && base + loader_key < k1;
-    const uint64_t gone = __ballot(!there), any_none = __ballot(none && there);
-    if (lane == 0) v.flags[wave] = (gone != 0) | (any_none != 0) << 1;
-    if (!(gone | any_none)) return;
-    if (lane == 0) v.gone[wave] = gone;
-    constexpr int kEach = ValueChunk::kWords / kScales;
-#pragma unroll
-    for (int s = 0; s < kScales; ++s) {
-      const bool nan = vc.scale[s] == 255, zero = nan || !there;
-      const uint64_t none_here = __ballot(nan && there);
-      if (lane == 0) v.none[s][wave] = none_here;
-      if (zero) vc.scale[s] = 0;
-#pragma unroll
-      for (int w = 0; w < kEach; ++w) vc.w[s * kEach + w] = zero ? 0 : vc.w[s * kEach + w];
-    }
-  };
-  const auto store_values = [&](int turn, int st) {
-    *reinterpret_cast<at_b8*>(shared.values[turn].rows + loader_key * kValueRow + part * 16 * kChunk + 16 * st) = vc.values(st);
-  };
-
-  float m = -INFINITY, l = 0.0f, most = -INFINITY;
+  float m, l;
   at_f16 o[DB];
+  // Goes through the keys of the run, HALF: with float16 values; false: float16 does not hold some of them
+  const auto go_through = [&]<bool HALF>() -> bool {
+    // Values of a tile before they go to LDS.  What has no place, and what is NaN, is zero there: a probability of zero does not take a NaN away
+    const auto prepare_values = [&](int turn, int base, bool page_there) {
+      Values& v = shared.values[turn];
+      constexpr int kScales = ValueChunk::kScales;
+      // scales between which nothing has to be looked at: float16 holds their blocks, or they are no NaN
+      constexpr uint32_t kLow = HALF ? 127 + narrow_low(VF) - kValuesUp : 0, kHigh = HALF ? 127 + narrow_high(VF) - kValuesUp : 254;
+      if (EVEN) vc.unpack(value_shift);
+      bool look = false;
 #pragma unroll
-  for (int d = 0; d < DB; ++d) o[d] = at_f16{};
-  // S^T: keys 32 i + 8 (e / 4) + 4 half + e % 4 of query lane % 32, element 16 i + e of a lane's 32.
-  struct Scores {
-    at_f16 s[2];
-  };
-  const auto key_of = [&](int turn, int k) {  // operand k of the scores' products: keys 32 (k % 2) on, columns 16 (k / 2) on
-    return *reinterpret_cast<const at_b8*>(shared.keys[turn] + (32 * (k % 2) + (lane & 31)) * kKeyRow + 32 * (k / 2) + 16 * half);
-  };
-  const auto score = [&](Scores& s, int k, const at_b8& key) {
-    if (k < 2) s.s[k] = at_f16{};
+      for (int s = 0; s < kScales; ++s) look |= vc.scale[s] - kLow > kHigh - kLow;
+      const bool there = page_there && base + loader_key < k1;
+      const uint64_t gone = __ballot(!there), any_look = __ballot(look && there);
+      if (lane == 0) v.flags[wave] = gone != 0;
+      if (!(gone | any_look)) return;
+      if (lane == 0) v.gone[wave] = gone;
+      constexpr int kEach = ValueChunk::kWords / kScales;
+      bool any_none = false, any_wide = false;
 #pragma unroll
-    for (int p = PIECES - 1; p >= 0; --p) s.s[k % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[p][k / 2], s.s[k % 2], 0, 0, 0);
-  };
-  const auto value_of = [&](int turn, int k) {  // operand k of the results' products: keys 16 (k / DB) on, columns 32 (k % DB) on
-    union {
-      at_s4 half[2];
-      at_b8 whole;
-    } v;
-    const uint8_t* from = shared.values[turn].rows + (4 * half + (lane & 15) / 4) * kValueRow + 2 * ((lane & 16) + 4 * (lane & 3)) + 16 * (k / DB) * kValueRow + 64 * (k % DB);
-    v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)from);
-    v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)(from + 8 * kValueRow));
-    return v.whole;
-  };
-  const auto most_of = [&](const Scores& s) {
-    float most = s.s[0][0];
+      for (int s = 0; s < kScales; ++s) {
+        const bool nan = vc.scale[s] == 255, zero = nan || !there;
+        const uint64_t none_here = __ballot(nan && there);
+        any_none |= none_here != 0;
+        if (lane == 0) v.none[s][wave] = none_here;
+        if (HALF) {
+          uint32_t bits = 0;
 #pragma unroll
-    for (int e = 1; e < 32; ++e) most = fmaxf(most, s.s[e / 16][e % 16]);
-    return most;
-  };
-  const auto seen_by_wave = [&](int base) { return base < wave_end && base + kTile > wave_low; };
-  const auto all_scores = [&](int turn, Scores& s) {
+          for (int w = 0; w < kEach; ++w) bits |= vc.w[s * kEach + w];
+          any_wide |= __ballot(!zero && vc.scale[s] - kLow > kHigh - kLow && (bits & (VF == kMxFp4 ? 0x77777777u : 0x7f7f7f7fu)) != 0) != 0;
+        }
+        if (zero) vc.scale[s] = 0;
 #pragma unroll
-    for (int k = 0; k < kProducts; ++k) score(s, k, key_of(turn, k));
-  };
-  bool values_there = false, keys_there = false;
-  int64_t next_place = 0;
-  // values of the next tile and keys of the one after it into LDS, those behind them under way; in kForward parts
-  constexpr int kForward = 2 * kChunk + 1;
-  const auto forward = [&](int turn, int base, int k) {
-    if (k == 0) prepare_values(turn ^ 1, base + kTile, values_there);
-    if (k >= 1 && k <= kChunk) store_values(turn ^ 1, k - 1);
-    if (k > kChunk && k <= 2 * kChunk) store_keys(turn, k - 1 - kChunk);
-  };
-  const auto load_next = [&](int base) {
-    values_there = keys_there;
-    load_values(next_place);
-    next_place = place_of(base + 3 * kTile, keys_there);
-    load_keys(next_place);
-    look_up(base + 4 * kTile);
-  };
-  // Tile `base`, whose scores and their largest are there: its share of the results; and the scores of the next one.  In the order that it is written in
-  // (the fences hold the compiler to it): operands are read kAhead products ahead, the next tile's scores alternate with this one's
-  // exponentials, this one's results with what is under way and the next one's maximum.
-  const auto step = [&](int base, int turn, Scores& s, Scores& next) {
-    const Values& b = shared.values[turn];
-    if (seen_by_wave(base)) {
-      at_b8 keys[kAhead], values[kAhead];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) keys[k] = key_of(turn ^ 1, k);
-      const uint64_t flags64 = *reinterpret_cast<const uint64_t*>(b.flags);
-      const auto next_score = [&](int k) {
-        score(next, k, keys[k % kAhead]);
-        if (k + kAhead < kProducts) keys[k % kAhead] = key_of(turn ^ 1, k + kAhead);
-        else values[k % kAhead] = value_of(turn, k + kAhead - kProducts);
-      };
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int k = 0; k < kLead; ++k) {
-        next_score(k);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int w = 0; w < kEach; ++w) vc.w[s * kEach + w] = zero ? 0 : vc.w[s * kEach + w];
       }
-      const uint32_t flags = __builtin_amdgcn_readfirstlane((uint32_t)flags64 | (uint32_t)(flags64 >> 32));
-      const bool any_gone = flags & 0x01010101, any_none = flags & 0x02020202;
+      if (lane == 0) v.flags[wave] = (gone != 0) | any_none << 1 | any_wide << 2;
+    };
+    const auto store_values = [&](int turn, int st) {
+      uint8_t* const to = shared.values[turn].rows + loader_key * kValueRow + part * 16 * kChunk + 16 * st;
+      if constexpr (HALF) *reinterpret_cast<at_h8*>(to) = attention_halves8<VF>(vc.words(st), vc.scale_of(st, kValuesUp));
+      else *reinterpret_cast<at_b8*>(to) = vc.values(st);
+    };
+
+    m = -INFINITY, l = 0.0f;
+    float most = -INFINITY;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = at_f16{};
+    // S^T: keys 32 i + 8 (e / 4) + 4 half + e % 4 of query lane % 32, element 16 i + e of a lane's 32.
+    struct Scores {
+      at_f16 s[2];
+    };
+    const auto key_of = [&](int turn, int k) {  // operand k of the scores' products: keys 32 (k % 2) on, columns 16 (k / 2) on
+      return *reinterpret_cast<const at_b8*>(shared.keys[turn] + (32 * (k % 2) + (lane & 31)) * kKeyRow + 32 * (k / 2) + 16 * half);
+    };
+    const auto score = [&](Scores& s, int k, const at_b8& key) {
+      if (k < 2) s.s[k] = at_f16{};
+#pragma unroll
+      for (int p = PIECES - 1; p >= 0; --p) s.s[k % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[p][k / 2], s.s[k % 2], 0, 0, 0);
+    };
+    const auto value_of = [&](int turn, int k) {  // operand k of the results' products: keys 16 (k / DB) on, columns 32 (k % DB) on
+      union {
+        at_s4 half[2];
+        at_b8 whole;
+      } v;
+      const uint8_t* from = shared.values[turn].rows + (4 * half + (lane & 15) / 4) * kValueRow + 2 * ((lane & 16) + 4 * (lane & 3)) + 16 * (k / DB) * kValueRow + 64 * (k % DB);
+      v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)from);
+      v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds_s4*)(from + 8 * kValueRow));
+      return v.whole;
+    };
+    const auto result = [&](at_f16& sum, const at_b8& value, const mx_u4& p) {
+      if constexpr (HALF) sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(at_h8, value), __builtin_bit_cast(at_h8, p), sum, 0, 0, 0);
+      else sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, __builtin_bit_cast(at_b8, p), sum, 0, 0, 0);
+    };
+    const auto most_of = [&](const Scores& s) {
+      float most = s.s[0][0];
+#pragma unroll
+      for (int e = 1; e < 32; ++e) most = fmaxf(most, s.s[e / 16][e % 16]);
+      return most;
+    };
+    const auto seen_by_wave = [&](int base) { return base < wave_end && base + kTile > wave_low; };
+    const auto all_scores = [&](int turn, Scores& s) {
+#pragma unroll
+      for (int k = 0; k < kProducts; ++k) score(s, k, key_of(turn, k));
+    };
+    bool values_there = false, keys_there = false;
+    int64_t next_place = 0;
+    // values of the next tile and keys of the one after it into LDS, those behind them under way; in kForward parts
+    constexpr int kForward = 2 * kChunk + 1;
+    const auto forward = [&](int turn, int base, int k) {
+      if (k == 0) prepare_values(turn ^ 1, base + kTile, values_there);
+      if (k >= 1 && k <= kChunk) store_values(turn ^ 1, k - 1);
+      if (k > kChunk && k <= 2 * kChunk) store_keys(turn, k - 1 - kChunk);
+    };
+    const auto load_next = [&](int base) {
+      values_there = keys_there;
+      load_values(next_place);
+      next_place = place_of(base + 3 * kTile, keys_there);
+      load_keys(next_place);
+      look_up(base + 4 * kTile);
+    };
+    // what a tile's rows do not see is minus infinity; the largest of the rest
+    const auto hide = [&](int base, const Values& b, Scores& s, bool any_gone) {
       if (base < wave_all_low || base + kTile > wave_all_end || any_gone) {
         const int from = low - base, to = end - base;
         uint64_t seen = from >= kTile || to <= 0 || from >= to ? 0 : (from <= 0 ? ~0ull : ~0ull << from) & (to >= kTile ? ~0ull : ~(~0ull << to));
@@ -323,11 +353,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
             if (!((uint32_t)(seen >> (32 * i)) >> (8 * (e / 4) + e % 4) & 1)) s.s[i][e] = -INFINITY;
         most = pair_max(most_of(s));
       }
-      // the maximum is raised only where scores are 2^kSlack times beyond it: the sums hold that
-      constexpr float kSlack = 6.0f;
+    };
+    const auto raise = [&] {
+      // m, 2^kDown below the maximum, is raised only where scores are 2^kSlack times beyond that: the sums hold it
+      constexpr float kDown = HALF ? kHead : 0.0f, kSlack = HALF ? 2.0f : 6.0f;
       most *= factor;
-      if (__ballot(most > m + kSlack)) {
-        const float raised = fmaxf(m, most), fade = raised == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - raised);
+      if (__ballot(most - m > kDown + kSlack)) {
+        // (of maxima beyond 2^16 the difference would be rounded)
+        const float raised = fmaxf(m, fabsf(most) < 0x1p16f ? most - kDown : most), fade = raised == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - raised);
         m = raised;
         l *= fade;
 #pragma unroll
@@ -335,162 +368,254 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[d][e] *= fade;
       }
+    };
+    // The product in the exponent is not rounded, the maximum's was: half a step of m apart, which 2^16 keeps at 2^-8.  Larger scores are rounded like the maximum.  What they are to
+    // be multiplied by, and what is added
+    const auto exponent = [&](Scores& s) -> float2 {
       const float zero = m == -INFINITY ? 0.0f : -m;
-      // The product in the exponent is not rounded, the maximum's was: half a step of m apart, which 2^16 keeps at 2^-8.  Larger scores are rounded like the maximum.
       const bool far = __ballot(fabsf(zero) >= 0x1p16f);
       if (far) [[unlikely]] {
 #pragma unroll
         for (int e = 0; e < 32; ++e) s.s[e / 16][e % 16] *= factor;
       }
       const float times = far ? 1.0f : factor;
-      mx_u4 pr[PROBABILITIES][4];
-      float x[2];
-      const auto exponentials = [&](int e) {  // elements e and e + 1
+      return make_float2(times, zero);
+    };
+    // NaN for the queries that see such a value, and for no other: block d lies in part d PARTS / DB
+    const auto set_none = [&](int base, const Values& b) {
+      constexpr int kScales = ValueChunk::kScales;
+      for (int at = 0; at < kTile; ++at) {
+        if (!(b.flags[at / kKeysAWave] & 2)) continue;
+        uint32_t bits[kScales], any = 0;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s.s[(e + j) / 16][(e + j) % 16], times, zero));
-        asm volatile("" : "+v"(x[0]), "+v"(x[1]));  // (here, not where they are used)
-      };
-      const auto probabilities = [&](int e) {
-        l += x[0] + x[1];
-        __bf16 piece[2][PROBABILITIES];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) attention_split<PROBABILITIES>(x[j], piece[j]);
-#pragma unroll
-        for (int k = 0; k < PROBABILITIES; ++k) {
-          uint32_t pair = __builtin_bit_cast(uint32_t, at_b2{piece[0][k], piece[1][k]});
-          asm volatile("" : "+v"(pair), "+v"(l));
-          pr[k][e / 8][e % 8 / 2] = pair;
+        for (int x = 0; x < kScales; ++x) {
+          bits[x] = (uint32_t)(b.none[x][at / kKeysAWave] >> (PARTS * (at % kKeysAWave))) & ((1 << PARTS) - 1);
+          any |= bits[x];
         }
-      };
-      // share k of kProducts of the 32 elements: the last pair's probabilities, the next pair's exponentials
-      const auto some = [&](int k) {
+        if (!any) continue;
+        const bool seen = base + at >= low && base + at < end;
 #pragma unroll
-        for (int e = 32 * k / kProducts; e < 32 * (k + 1) / kProducts; ++e)
-          if (e % 2) {
-            if (e > 1) probabilities(e - 3);
-            exponentials(e - 1);
-          }
-      };
-      // a wavefront that has its exponentials under way goes first on its SIMD: the two are not at the same place then (prompt of 8192 579 -> 566 us)
-      __builtin_amdgcn_s_setprio(1);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int d = 0; d < DB; ++d) {
+          const bool nan = bits[d % kScales] >> (d * PARTS / DB) & 1;
 #pragma unroll
-      for (int k = kLead; k < kProducts; ++k) {
-        next_score(k);
-        some(k - kLead);
+          for (int e = 0; e < 16; ++e) o[d][e] = nan && seen ? NAN : o[d][e];
+        }
+      }
+    };
+    // Tile `base`, whose scores and their largest are there: its share of the results; and the scores of the next one.  In the order that it is written in
+    // (the fences hold the compiler to it): operands are read kAhead products ahead, the next tile's scores alternate with this one's
+    // exponentials, this one's results with what is under way and the next one's maximum.
+    const auto step = [&](int base, int turn, Scores& s, Scores& next) {
+      const Values& b = shared.values[turn];
+      const uint64_t flags64 = *reinterpret_cast<const uint64_t*>(b.flags);
+      const auto any_flag = [&] { return __builtin_amdgcn_readfirstlane((uint32_t)flags64 | (uint32_t)(flags64 >> 32)); };
+      uint32_t flags;
+      if (seen_by_wave(base)) {
+        at_b8 keys[kAhead], values[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) keys[k] = key_of(turn ^ 1, k);
+        const auto next_score = [&](int k) {
+          score(next, k, keys[k % kAhead]);
+          if (k + kAhead < kProducts) keys[k % kAhead] = key_of(turn ^ 1, k + kAhead);
+          else values[k % kAhead] = value_of(turn, k + kAhead - kProducts);
+        };
         __builtin_amdgcn_sched_barrier(0);
-      }
-      most = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < kProducts; ++k) {
-        const int u = k / DB, d = k % DB;
-#pragma unroll
-        for (int p = PROBABILITIES - 1; p >= 0; --p) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values[k % kAhead], __builtin_bit_cast(at_b8, pr[p][u]), o[d], 0, 0, 0);
-        if (k + kAhead < kProducts) values[k % kAhead] = value_of(turn, k + kAhead);
-        if (k < kLead) some(k + kProducts - kLead);
-        if (k == kLead) probabilities(30);
-        if (k >= kLead) {
-          constexpr int kRest = kProducts - kLead;
-          const int at = k - kLead;
-#pragma unroll
-          for (int f = kForward * at / kRest; f < kForward * (at + 1) / kRest; ++f) forward(turn, base, f);
-#pragma unroll
-          for (int e = 32 * at / kRest; e < 32 * (at + 1) / kRest; ++e) most = fmaxf(most, next.s[e / 16][e % 16]);
-          asm volatile("" : "+v"(most));
+        for (int k = 0; k < kLead; ++k) {
+          next_score(k);
+          __builtin_amdgcn_sched_barrier(0);
         }
+        flags = any_flag();
+        const bool any_gone = flags & 0x01010101, any_none = flags & 0x02020202;
+        hide(base, b, s, any_gone);
+        raise();
+        const auto [times, zero] = exponent(s);
+        constexpr int kPieces = HALF ? 1 : 2;
+        mx_u4 pr[kPieces][4];
+        float x[2];
+        const auto exponentials = [&](int e) {  // elements e and e + 1
+#pragma unroll
+          for (int j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s.s[(e + j) / 16][(e + j) % 16], times, zero));
+          asm volatile("" : "+v"(x[0]), "+v"(x[1]));  // (here, not where they are used)
+        };
+        const auto probabilities = [&](int e) {
+          l += x[0] + x[1];
+          __bf16 piece[2][kPieces];
+          if constexpr (!HALF) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) attention_split<kPieces>(x[j], piece[j]);
+          }
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) {
+            uint32_t pair = HALF ? __builtin_bit_cast(uint32_t, at_h2{(_Float16)x[0], (_Float16)x[1]}) : __builtin_bit_cast(uint32_t, at_b2{piece[0][k], piece[1][k]});
+            asm volatile("" : "+v"(pair), "+v"(l));
+            pr[k][e / 8][e % 8 / 2] = pair;
+          }
+        };
+        // share k of kProducts of the 32 elements: the last pair's probabilities, the next pair's exponentials
+        const auto some = [&](int k) {
+#pragma unroll
+          for (int e = 32 * k / kProducts; e < 32 * (k + 1) / kProducts; ++e)
+            if (e % 2) {
+              if (e > 1) probabilities(e - 3);
+              exponentials(e - 1);
+            }
+        };
+        // a wavefront that has its exponentials under way goes first on its SIMD: the two are not at the same place then (prompt of 8192 579 -> 566 us)
+        __builtin_amdgcn_s_setprio(1);
         __builtin_amdgcn_sched_barrier(0);
-      }
-      __builtin_amdgcn_s_setprio(0);
-      most = pair_max(most);
-      if (any_none) {
-        // NaN for the queries that see such a value, and for no other: block d lies in part d PARTS / DB
-        constexpr int kScales = ValueChunk::kScales;
-        for (int at = 0; at < kTile; ++at) {
-          if (!(b.flags[at / kKeysAWave] & 2)) continue;
-          uint32_t bits[kScales], any = 0;
 #pragma unroll
-          for (int x = 0; x < kScales; ++x) {
-            bits[x] = (uint32_t)(b.none[x][at / kKeysAWave] >> (PARTS * (at % kKeysAWave))) & ((1 << PARTS) - 1);
-            any |= bits[x];
-          }
-          if (!any) continue;
-          const bool seen = base + at >= low && base + at < end;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const bool nan = bits[d % kScales] >> (d * PARTS / DB) & 1;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[d][e] = nan && seen ? NAN : o[d][e];
-          }
+        for (int k = kLead; k < kProducts; ++k) {
+          next_score(k);
+          some(k - kLead);
+          __builtin_amdgcn_sched_barrier(0);
         }
+        most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kProducts; ++k) {
+          const int u = k / DB, d = k % DB;
+#pragma unroll
+          for (int p = kPieces - 1; p >= 0; --p) result(o[d], values[k % kAhead], pr[p][u]);
+          if (k + kAhead < kProducts) values[k % kAhead] = value_of(turn, k + kAhead);
+          if (k < kLead) some(k + kProducts - kLead);
+          if (k == kLead) probabilities(30);
+          if (k >= kLead) {
+            constexpr int kRest = kProducts - kLead;
+            const int at = k - kLead;
+#pragma unroll
+            for (int f = kForward * at / kRest; f < kForward * (at + 1) / kRest; ++f) forward(turn, base, f);
+#pragma unroll
+            for (int e = 32 * at / kRest; e < 32 * (at + 1) / kRest; ++e) most = fmaxf(most, next.s[e / 16][e % 16]);
+            asm volatile("" : "+v"(most));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        most = pair_max(most);
+        if (any_none) set_none(base, b);
+      } else {
+        flags = any_flag();
+        if (seen_by_wave(base + kTile)) {
+          all_scores(turn ^ 1, next);
+          most = pair_max(most_of(next));
+        }
+#pragma unroll
+        for (int k = 0; k < kForward; ++k) forward(turn, base, k);
       }
-    } else {
-      if (seen_by_wave(base + kTile)) {
-        all_scores(turn ^ 1, next);
-        most = pair_max(most_of(next));
+      load_next(base);
+      __syncthreads();
+      return !HALF || !(flags & 0x04040404);  // (the same in all wavefronts)
+    };
+    // The same for values that float16 does not hold.
+    const auto plain_step = [&](int base, int turn) {
+      const Values& b = shared.values[turn];
+      const bool seen = seen_by_wave(base);
+      Scores s;
+      if (seen) {
+        all_scores(turn, s);
+        most = pair_max(most_of(s));
       }
+      __syncthreads();  // (what follows writes over these keys)
 #pragma unroll
       for (int k = 0; k < kForward; ++k) forward(turn, base, k);
-    }
-    load_next(base);
-    __syncthreads();
-  };
+      if (seen) {
+        const uint64_t flags64 = *reinterpret_cast<const uint64_t*>(b.flags);
+        const uint32_t flags = __builtin_amdgcn_readfirstlane((uint32_t)flags64 | (uint32_t)(flags64 >> 32));
+        hide(base, b, s, flags & 0x01010101);
+        raise();
+        const auto [times, zero] = exponent(s);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          at_b8 p[2];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s.s[u / 2][8 * (u % 2) + j], times, zero));
+            l += x;
+            __bf16 piece[2];
+            attention_split<2>(x, piece);
+            p[0][j] = piece[0], p[1][j] = piece[1];
+          }
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const at_b8 v = value_of(turn, u * DB + d);
+#pragma unroll
+            for (int k = 1; k >= 0; --k) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], o[d], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (flags & 0x02020202) set_none(base, b);
+      }
+      load_next(base);
+      __syncthreads();
+    };
 
-  Scores even, odd;
-  if (k0 < k1) {
-    if (threadIdx.x < 16) shared.values[threadIdx.x / 8].flags[threadIdx.x % 8] = 0;  // (of wavefronts that there are not, too)
-    __syncthreads();
-    // what does not wait for one another, together
-    int32_t pages[4];
+    if (k0 < k1) {
+      if (threadIdx.x < 16) shared.values[threadIdx.x / 8].flags[threadIdx.x % 8] = 0;  // (of wavefronts that there are not, too)
+      __syncthreads();
+      // what does not wait for one another, together
+      int32_t pages[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      look_up(k0 + j * kTile);
-      pages[j] = next_page;
-    }
-    KeyChunk early[2];
-    ValueChunk first;
-    bool early_there = false;
+      for (int j = 0; j < 4; ++j) {
+        look_up(k0 + j * kTile);
+        pages[j] = next_page;
+      }
+      KeyChunk early[2];
+      ValueChunk first;
+      bool early_there = false;
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
-      next_page = pages[j];
-      next_place = place_of(k0 + j * kTile, j == 0 ? early_there : j == 1 ? values_there : keys_there);
-      load_keys(next_place);
-      if (j < 2) load_values(next_place);
-      if (j < 2) early[j] = kc;
-      if (j == 0) first = vc;
-    }
-    next_page = pages[3];
-    const KeyChunk last = kc;
-    const ValueChunk second = vc;
-    vc = first;
-    prepare_values(0, k0, early_there);
+      for (int j = 0; j < 3; ++j) {
+        next_page = pages[j];
+        next_place = place_of(k0 + j * kTile, j == 0 ? early_there : j == 1 ? values_there : keys_there);
+        load_keys(next_place);
+        if (j < 2) load_values(next_place);
+        if (j < 2) early[j] = kc;
+        if (j == 0) first = vc;
+      }
+      next_page = pages[3];
+      const KeyChunk last = kc;
+      const ValueChunk second = vc;
+      vc = first;
+      prepare_values(0, k0, early_there);
 #pragma unroll
-    for (int st = 0; st < kChunk; ++st) store_values(0, st);
+      for (int st = 0; st < kChunk; ++st) store_values(0, st);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      kc = early[j];
+      for (int j = 0; j < 2; ++j) {
+        kc = early[j];
 #pragma unroll
-      for (int st = 0; st < kChunk; ++st) store_keys(j, st);
+        for (int st = 0; st < kChunk; ++st) store_keys(j, st);
+      }
+      kc = last;
+      vc = second;
+      __syncthreads();
+      if constexpr (!HALF && many_halves(TYPE, DB)) {
+        for (int base = k0; base < k1; base += 2 * kTile) {
+          plain_step(base, 0);
+          if (base + kTile < k1) plain_step(base + kTile, 1);
+        }
+      } else {
+        Scores even, odd;
+        if (seen_by_wave(k0)) {
+          all_scores(0, even);
+          most = pair_max(most_of(even));
+        }
+        __syncthreads();  // (the first step writes over these keys)
+        for (int base = k0; base < k1; base += 2 * kTile) {
+          if (!step(base, 0, even, odd)) return false;
+          if (base + kTile < k1 && !step(base + kTile, 1, odd, even)) return false;
+        }
+      }
     }
-    kc = last;
-    vc = second;
-    __syncthreads();
-    if (seen_by_wave(k0)) {
-      all_scores(0, even);
-      most = pair_max(most_of(even));
-    }
-    __syncthreads();  // (the first step writes over these keys)
-    for (int base = k0; base < k1; base += 2 * kTile) {
-      step(base, 0, even, odd);
-      if (base + kTile < k1) step(base + kTile, 1, odd, even);
-    }
-  }
+    return true;
+  };
+  const bool half_values = many_halves(TYPE, DB) && go_through.template operator()<many_halves(TYPE, DB)>();
+  if (!half_values) (void)go_through.template operator()<false>();
 
   // a lane has columns 32 d + 8 i + 4 half .. + 3 of its query
-  const float sum = pair_sum(l);
+  const float sum = pair_sum(l), back = half_values ? 1.0f / (1 << kValuesUp) : 1.0f;
   if (!row_there) return;
   const int64_t out_row = (int64_t)(span.first + token) * a.heads + q_head;
   if (run.runs == 1) {
-    const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const float inverse = sum > 0.0f || sum != sum ? back / sum : 0.0f;
     E* out = static_cast<E*>(a.out) + out_row * c.dim;
     typedef E elements __attribute__((ext_vector_type(4)));
     typedef elements elements_any __attribute__((aligned(sizeof(E))));
@@ -523,7 +648,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<at_f4*>(work.partial + (slot * ROWS + row) * D + 32 * d + 8 * i + 4 * half) = at_f4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+      *reinterpret_cast<at_f4*>(work.partial + (slot * ROWS + row) * D + 32 * d + 8 * i + 4 * half) = at_f4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * back;
   if (half == 0) {
     work.stats[slot * ROWS + row] = make_float2(m, sum);
     if (split == 0) work.joins[out_row] = make_int2((int)(first * ROWS + row), run.runs);
