@@ -13,7 +13,7 @@
 // bfloat16 numbers for bfloat16 queries too: one would be 2^-8 off, as much as the result's own rounding, and the second costs 0 to 2.5 % where bytes bound the kernel
 // (the 64 sequences below 148.1 and 148.6 us, their 4-bit codes 89.1 and 91.5).
 //
-// 64 sequences of 1024 to 16384 tokens, 32 heads over 8 of 128 columns, 8-bit codes: 146 us with the join's 7, 5.1 TB/s of 752 MB (a copy has 5.9); 4-bit codes 88 us.  One
+// 64 sequences of 1024 to 16384 tokens, 32 heads over 8 of 128 columns, 8-bit codes: 147 us with the join's 7, 5.1 TB/s of 752 MB (a copy has 5.9); 4-bit codes 92 us.  One
 // token over 1000 keys 9.5 us, 6.5 and 3.8 of them the two kernels: launches, and three rounds of memory in the first.
 #include "mx_attention.h"
 
@@ -390,14 +390,15 @@ __global__ __launch_bounds__(kThreads) void join_kernel(CacheArgs c, AttentionAr
 }
 
 // Which kernel: the one for many rows where a sequence has more than two tiles of sixteen on the average, queries of all heads that share keys (the number of rows of
-// each is not known here).  16 sequences of 4096, 16, 32, 48, 64 and 128 rows of 128 columns, us: bfloat16 44, 57, 76, 85, 152 here and 56, 60, 58, 60, 71 there; float16 51, 66,
-// 86, 95, 159 and 72, 75, 76, 76, 94.  Short sequences gain later: 64 chunks of 64 rows with nothing before them 28 and 38, of 256 rows 76 and 47.
+// each is not known here).  16 sequences of 4096, 16, 32, 48, 64 and 128 rows of 128 columns, us: bfloat16 47, 60, 78, 87, 151 here and 56, 60, 58, 60, 71 there; float16 53, 68,
+// 88, 95, 160 and 71, 73, 74, 75, 92.  Short sequences gain later: 64 chunks of 64 rows with nothing before them 26 and 38, of 256 rows 75 and 46.  One chunk of 512 tokens over 32768 and
+// 128 single tokens over 1024, 20 rows on the average, take 999 here (296 and 72 each by itself).
 // binary32 queries take three products for one and have the kernel here alone.
 constexpr int64_t kManyRowsFrom = 33;
 bool many_rows(const AttentionArgs& a, const CacheArgs& c) { return (int64_t)a.T * (a.heads / c.kv_heads) >= kManyRowsFrom * c.seqs; }
 
 // More sequences are planned by a launch in front.  With every workgroup looking at all of them, tokens over 512 sequences of 512, 2048 of 1024 and 4096 of 64 keys took 152, 1172 and
-// 1973 us; so 115, 770 and 272, and the launch 5 of those.
+// 1973 us; so 115, 770 and 276, and the launch 5 of those.
 constexpr int64_t kMostScanned = 256;
 
 constexpr int64_t padded16(int64_t n) { return (n + 15) / 16 * 16; }

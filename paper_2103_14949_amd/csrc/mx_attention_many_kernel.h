@@ -6,9 +6,9 @@
 // query's scores in two lanes' registers, as the operand of O^T = V^T P^T, so that the softmax needs one lane exchange and nothing of it goes
 // through LDS; values are read transposed from there.  The next tile's scores are worked out beside this tile's exponentials, in the order that is written.
 //
-// Eight wavefronts of 32 rows share a CU, two a SIMD, up to 128 columns of bfloat16; four where 256 registers do not do.  Prompt of 8192, 32 heads over 8 of 128 columns: 540 to 566 us,
-// 970 to 1020 TFLOP/s (a product of 8192 x 8192 x 8192 has 1480, of 16384 1600), matrix unit 44 % of the cycles at 2 GHz, vector instructions 56 %; a chunk of 1024 over 32768 503 to 528 us; 256 columns
-// 595 TFLOP/s, float16 queries 430.  Tried and slower: 64 rows a wavefront, whose sums the compiler copies between register files (1020 us); three tiles in LDS and the
+// Eight wavefronts of 32 rows share a CU, two a SIMD, up to 128 columns of bfloat16; four where 256 registers do not do.  Prompt of 8192, 32 heads over 8 of 128 columns: 554 to 575 us,
+// 960 to 990 TFLOP/s (a product of 8192 x 8192 x 8192 has 1480, of 16384 1600), matrix unit 44 % of the cycles at 2 GHz, vector instructions 57 %: the two hardly overlap; a chunk of 1024 over 32768 529 to
+// 550 us; 256 columns 850 us, 645 TFLOP/s, float16 queries 1030 to 1055, 525 TFLOP/s.  Tried and slower: 64 rows a wavefront, whose sums the compiler copies between register files (1020 us); three tiles in LDS and the
 // first operands read in front of the barrier (registers: 595 for 555); eight operands ahead (660 for 590).  LDS is not what bounds it: half the operand reads, on the same
 // data twice, 634 us for 652.
 #pragma once
