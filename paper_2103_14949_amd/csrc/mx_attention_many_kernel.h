@@ -6,9 +6,9 @@
 // query's scores in two lanes' registers, as the operand of O^T = V^T P^T, so that the softmax needs one lane exchange and nothing of it goes
 // through LDS; values are read transposed from there.  The next tile's scores are worked out beside this tile's exponentials, in the order that is written.
 //
-// Eight wavefronts of 32 rows share a CU, two a SIMD, up to 128 columns of bfloat16; four where 256 registers do not do.  Prompt of 8192, 32 heads over 8 of 128 columns: 554 to 575 us,
-// 960 to 990 TFLOP/s (a product of 8192 x 8192 x 8192 has 1480, of 16384 1600), matrix unit 44 % of the cycles at 2 GHz, vector instructions 57 %: the two hardly overlap; a chunk of 1024 over 32768 529 to
-// 550 us; 256 columns 850 us, 645 TFLOP/s, float16 queries 1030 to 1055, 525 TFLOP/s.  Tried and slower: 64 rows a wavefront, whose sums the compiler copies between register files (1020 us); three tiles in LDS and the
+// Eight wavefronts of 32 rows share a CU, two a SIMD, up to 128 columns of bfloat16; four where 256 registers do not do.  Prompt of 8192, 32 heads over 8 of 128 columns: 544 to 575 us,
+// 955 to 1010 TFLOP/s (a product of 8192 x 8192 x 8192 has 1480, of 16384 1600), matrix unit 44 % of the cycles at 2 GHz, vector instructions 57 %: the two hardly overlap; a chunk of 1024 over 32768 517 to
+// 550 us; 256 columns 835 to 855 us, 645 TFLOP/s, float16 queries 1020 to 1055, 530 TFLOP/s.  Tried and slower: 64 rows a wavefront, whose sums the compiler copies between register files (1020 us); three tiles in LDS and the
 // first operands read in front of the barrier (registers: 595 for 555); eight operands ahead (660 for 590).  LDS is not what bounds it: half the operand reads, on the same
 // data twice, 634 us for 652.
 #pragma once
@@ -256,15 +256,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
       bool any_none = false, any_wide = false;
 #pragma unroll
       for (int s = 0; s < kScales; ++s) {
-        const bool nan = vc.scale[s] == 255, zero = nan || !there;
+        const bool nan = vc.scale[s] == 255;
+        bool zero = nan || !there;
         const uint64_t none_here = __ballot(nan && there);
         any_none |= none_here != 0;
         if (lane == 0) v.none[s][wave] = none_here;
         if (HALF) {
+          // (zeros are zeros whatever their scale, which 2^kValuesUp times may be none)
           uint32_t bits = 0;
 #pragma unroll
           for (int w = 0; w < kEach; ++w) bits |= vc.w[s * kEach + w];
-          any_wide |= __ballot(!zero && vc.scale[s] - kLow > kHigh - kLow && (bits & (VF == kMxFp4 ? 0x77777777u : 0x7f7f7f7fu)) != 0) != 0;
+          zero |= !(bits & (VF == kMxFp4 ? 0x77777777u : 0x7f7f7f7fu));
+          any_wide |= __ballot(!zero && vc.scale[s] - kLow > kHigh - kLow) != 0;
         }
         if (zero) vc.scale[s] = 0;
 #pragma unroll
@@ -359,8 +362,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void many_kernel(CacheArgs c
       constexpr float kDown = HALF ? kHead : 0.0f, kSlack = HALF ? 2.0f : 6.0f;
       most *= factor;
       if (__ballot(most - m > kDown + kSlack)) {
-        // (of maxima beyond 2^16 the difference would be rounded)
-        const float raised = fmaxf(m, fabsf(most) < 0x1p16f ? most - kDown : most), fade = raised == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - raised);
+        // (from larger maxima the difference may be rounded to 2^16 and more)
+        const float raised = fmaxf(m, fabsf(most) < 0x1p22f ? most - kDown : most), fade = raised == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - raised);
         m = raised;
         l *= fade;
 #pragma unroll

@@ -121,3 +121,21 @@ def test_none_and_beyond_float16_together():
 def test_many_rows_of_more_than_128_columns(new, lengths, dim):
     """Two bfloat16 numbers in the kernel for many rows: 2^-16."""
     assert off(new, lengths, 8, 4, dim, dim, 2.0 ** -16).max() <= 1
+
+
+@pytest.mark.parametrize("v_fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("sign", [0, 1])
+@pytest.mark.parametrize("byte", [0, 1, 128, 200, 245, 249, 250, 251, 254])
+def test_zeros_of_any_scale(byte, sign, v_fmt):
+    """A block of zeros, of either sign, stands for zeros whatever its scale is; a quarter of a block, too."""
+    rng = np.random.default_rng(byte)
+    table, lengths, offsets, pages = layout([70], [200], 16)
+    cache, keys, values = random_cache(rng, pages, 1, 16, 128, "fp8", v_fmt)
+    code = (0x88 if v_fmt == "fp4" else 0x80) if sign else 0
+    where = rng.random(cache.v_scales.shape) < 0.3
+    cache.v_scales[torch.from_numpy(where).to(DEV)] = byte
+    cache.v_codes[torch.from_numpy(np.repeat(where, cache.v_codes.shape[-1] // where.shape[-1], -1)).to(DEV)] = code
+    values[np.repeat(where, 32, -1)] = 0
+    q = torch.from_numpy(rng.standard_normal((70, 2, 128))).to(torch.bfloat16)
+    out = hago.mx_attention(q.to(DEV), cache, *on_gpu(table, lengths, offsets))
+    check_attention(out, "bf16", q.double().numpy(), keys, values, ref.Sequences(table, lengths, offsets, pages, 16), 128 ** -0.5)
