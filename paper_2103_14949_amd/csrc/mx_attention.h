@@ -1,6 +1,6 @@
 // What the kernels of the attention over a paged cache of microscaled keys and values have in common.
 //
-// Keys and values go into the matrix instructions as bfloat16, which holds every code times its scale (three bits of mantissa, the
+// Keys and values go into the matrix instructions as bfloat16 (values as float16 where the kernel for many rows says so), which holds every code times its scale (three bits of mantissa, the
 // exponents of binary32; below 2^-126 it may be zero); queries as one, two or three bfloat16 numbers that add up to theirs (bfloat16, float16, binary32), and probabilities
 // as each kernel says.  Sums are binary32.
 #pragma once
